@@ -289,7 +289,7 @@ def _plain_scan(s, c, mode):
     if mode == "forward":
         return out
     # g_t = dy_t + a_{t+1} g_{t+1}, the same recurrence from the end
-    dy = s["dy"].float()
+    dy = s["dy"].to(torch.float32, copy=True)
     dy[:, -1] += s["dh_out"]
     after = torch.cat((torch.zeros_like(a[:, :1]), a[:, 1:].flip(1)), dim=1)
     g = _linear_recurrence(after, dy.flip(1)).flip(1)

@@ -73,7 +73,9 @@ enum {
                                    work on one sequence at a time, the work cut evenly over the SMs */
     LASAD_OPT_PREFILL_CHUNK = 1,/* CUDA-core prefill chunk length: 0 auto, else 16/32/64          */
     LASAD_OPT_DECODE_TPU = 2,   /* decode: threads per (b,h) state; 0 auto, else 32/64/128/256 */
-    LASAD_OPT_WAIT_LIMIT = 3    /* iteration cap of device-side waits; 0 = library default   */
+    LASAD_OPT_WAIT_LIMIT = 3,   /* iteration cap of device-side waits; 0 = library default   */
+    LASAD_OPT_WINDOW_IMPL = 4   /* window attention and its gradient: 0 auto (bf16: 2, f32: 1), 1 CUDA cores,
+                                   2 tensor cores (bf16 only)                                */
 };
 
 typedef struct lasad_params {
@@ -269,6 +271,163 @@ int lasad_forward_fused(lasad_ctx* ctx, const lasad_params* p,
 int lasad_decode_step_fused(lasad_ctx* ctx, const lasad_params* p,
                             const void* q_pre, const void* k, const void* v, const void* gate_pre,
                             float* state, void* o, float norm_eps, void* cuda_stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * What stands beside LASAD in a hybrid stack: a recurrence with one state per channel, the norm and
+ * rotation of queries and keys, and softmax attention over a sliding window.  They take the same
+ * positions (t0, prefix_len, grid_w), the same dtypes, the same alignment of pointers and strides
+ * (16 bytes; lasad_scan_* only that of one element) and the same errors as the calls above, write
+ * every output they are given, and keep nothing between calls: what they need beside the outputs is
+ * the caller's `workspace` (16-byte aligned device memory of the size that the matching query
+ * returns; NULL where that is 0), which is free again once the stream has passed the call.  They
+ * allocate nothing, may be recorded into a CUDA graph, and give the same bits on every run.
+ * B <= 65535; f32 tensors may not be mixed with bf16 ones in one call.
+ * ---------------------------------------------------------------------------------------------- */
+
+/*
+ * Gated linear recurrence with the spatial rule, per batch element and channel:
+ *
+ *     h_t = a_t h_{t-1} + g_t x_t ,   y_t = h_t ,   h_{-1} = h_in ,
+ *
+ * a_t = 1 on a row-boundary step and lambda_t elsewhere (the SAD rule of Section 3.4 with a state of
+ * one value per channel); g_t = 1 - lambda_t with LASAD_SCAN_TIED (the base decay, lambda_t = 1 - k_t)
+ * and 1 without.  `gate` holds lambda in [0,1], or, with LASAD_SCAN_LOGITS, pre-activations whose
+ * sigmoid it is (and 1 - lambda then keeps its precision where lambda is close to 1).
+ * Any B, T, C >= 1; arithmetic, states and sums in fp32.
+ */
+enum { LASAD_SCAN_TIED = 1, LASAD_SCAN_LOGITS = 2 };
+enum { LASAD_SCAN_CHUNK = 128 }; /* tokens between two saved states */
+
+typedef struct lasad_scan_params {
+    int32_t B, T, C;
+    int32_t grid_w, prefix_len; /* as in lasad_params */
+    int32_t dtype;              /* of x, gate, y, dy, dx, dgate */
+    int32_t flags;              /* LASAD_SCAN_* */
+    int32_t reserved;           /* must be 0 */
+    int64_t t0;
+    /* element strides of (batch, token); channels are contiguous.  lasad_scan_step reads [0] only.
+       y_stride is dy's too. */
+    int64_t x_stride[2], gate_stride[2], y_stride[2], dx_stride[2], dgate_stride[2];
+} lasad_scan_params;
+
+/* Bytes of workspace of lasad_scan_forward and lasad_scan_backward, or a negative LASAD_ERR_*. */
+int64_t lasad_scan_workspace(lasad_ctx* ctx, const lasad_scan_params* p);
+/*
+ *   x, gate, y   [B,T,C]           h_in, h_out  [B,C] fp32 or NULL
+ *   saved        [B, ceil(T / LASAD_SCAN_CHUNK), C] fp32 or NULL: h before every chunk, which the
+ *                backward needs
+ */
+int lasad_scan_forward(lasad_ctx* ctx, const lasad_scan_params* p, const void* x, const void* gate,
+                       const float* h_in, void* y, float* h_out, float* saved, void* workspace, void* cuda_stream);
+/*
+ * The gradient: dy [B,T,C] and dh_out [B,C] fp32 (or NULL) to dx, dgate [B,T,C] (the gradient of
+ * lambda, or of the pre-activation) and dh_in [B,C] fp32 (or NULL).
+ */
+int lasad_scan_backward(lasad_ctx* ctx, const lasad_scan_params* p, const void* x, const void* gate,
+                        const float* saved, const void* dy, const float* dh_out, void* dx, void* dgate, float* dh_in,
+                        void* workspace, void* cuda_stream);
+/* One token: x, gate, y [B,C]; h_in, h_out [B,C] fp32 (may be the same memory).  pos [B] int32
+ * (device): each sequence's absolute position, or NULL for t0. */
+int lasad_scan_step(lasad_ctx* ctx, const lasad_scan_params* p, const void* x, const void* gate, const float* h_in,
+                    void* y, float* h_out, const int32_t* pos, void* cuda_stream);
+
+/*
+ * RMS norm of every head's query and key and their rotation by position, in one pass:
+ *
+ *     out = R(position) (weight * x / sqrt(mean(x^2) + eps)) .
+ *
+ * R turns pairs of channels, (2m, 2m + 1) or, with LASAD_ROPE_HALF, (m, m + d/2), by the angles of
+ * `table`: fp32 (cos, sin) pairs [table_rows, pairs, 2].  With grid_w = 0 there are d/2 pairs per row
+ * and token i takes row i.  With a grid there are d/4: the first d/4 pairs of a head take the row
+ * of the table that is the token's grid row, the others that of its column; the prefix_len tokens
+ * before the grid are not turned.  Token t of sequence b is at pos[b] + t (pos [B] int32, device)
+ * or t0 + t (pos NULL).  A position from t0 must lie in the table; one from pos that does not takes
+ * the table's last (or first) row.
+ *   q [B,T,Hq,d], k [B,T,Hk,d]; weights [d] fp32 or NULL (ones); d in {32, 64}; any Hq, Hk >= 1.
+ *   An output may be its own input.
+ */
+enum { LASAD_ROPE_HALF = 1 };
+
+typedef struct lasad_rope_params {
+    int32_t B, T, Hq, Hk, d;
+    int32_t dtype; /* of q, k and their outputs and gradients */
+    int32_t grid_w, prefix_len;
+    int32_t table_rows;
+    int32_t flags; /* LASAD_ROPE_* */
+    float eps;     /* >= 0 */
+    int32_t reserved;
+    int64_t t0;
+    /* element strides of (batch, token, head); the forward reads the first four, the backward the
+       inputs', the dq_out / dk_out (gradients of the outputs) and the dq / dk ones */
+    int64_t q_stride[3], k_stride[3], q_out_stride[3], k_out_stride[3];
+    int64_t dq_out_stride[3], dk_out_stride[3], dq_stride[3], dk_stride[3];
+} lasad_rope_params;
+
+int lasad_qk_norm_rope(lasad_ctx* ctx, const lasad_rope_params* p, const void* q, const void* k, const float* table,
+                       const float* q_weight, const float* k_weight, const int32_t* pos, void* q_out, void* k_out,
+                       void* cuda_stream);
+/* Bytes of workspace of the backward, or a negative LASAD_ERR_*. */
+int64_t lasad_qk_norm_rope_workspace(lasad_ctx* ctx, const lasad_rope_params* p);
+/* The gradient, from the forward's inputs and dq_out, dk_out: dq, dk, and dq_weight, dk_weight [d]
+ * fp32 (each or NULL; with both NULL no workspace is needed). */
+int lasad_qk_norm_rope_backward(lasad_ctx* ctx, const lasad_rope_params* p, const void* q, const void* k,
+                                const float* table, const float* q_weight, const float* k_weight, const int32_t* pos,
+                                const void* dq_out, const void* dk_out, void* dq, void* dk, float* dq_weight,
+                                float* dk_weight, void* workspace, void* cuda_stream);
+
+/*
+ * Causal softmax attention over a sliding window with first tokens that stay visible: token t sees
+ *
+ *     V(t) = { s <= t : t - s < window  or  s < sinks } ,
+ *     o_t = sum_{s in V(t)} p_ts v_s ,   p_ts = e^(scale q_t.k_s) / sum_{V(t)} e^(scale q_t.k_s) .
+ *
+ *   q, o [B,T,Hq,d], k, v [B,T,Hk,d], d in {32, 64}, Hk divides Hq (query head h reads key head
+ *   h / (Hq / Hk)), 1 <= window, 0 <= sinks <= 128.
+ *   lengths [B] int32 (device) or NULL: sequence b ends before token lengths[b] (0 to T).  A row
+ *   past the end is empty: its o and gradients are 0 and its lse is -infinity, and nothing that
+ *   stands in q, k, v, o, do there counts, not even a NaN.
+ *   lse [B,Hq,T] fp32: log of the row's sum of e^(scale q.k); may be NULL in the forward.
+ * With bf16 the products run on the tensor cores with fp32 accumulation, statistics and exponentials
+ * in fp32; the weights p and the gradients of the scores are rounded to bf16 where they enter a
+ * product.  With f32 everything is fp32.
+ */
+typedef struct lasad_window_params {
+    int32_t B, T, Hq, Hk, d; /* T: tokens (ignored by the step) */
+    int32_t dtype;
+    int32_t window, sinks;
+    float scale;
+    int32_t reserved;
+    /* element strides of (batch, token, head); [1] of the tensors of one token is not read.
+       The caches' are those of (batch, slot, head). */
+    int64_t q_stride[3], k_stride[3], v_stride[3], o_stride[3];
+    int64_t do_stride[3], dq_stride[3], dk_stride[3], dv_stride[3];
+    int64_t k_cache_stride[3], v_cache_stride[3];
+} lasad_window_params;
+
+int lasad_window_attention(lasad_ctx* ctx, const lasad_window_params* p, const void* q, const void* k, const void* v,
+                           const int32_t* lengths, void* o, float* lse, void* cuda_stream);
+/* Bytes of workspace of the backward, or a negative LASAD_ERR_*. */
+int64_t lasad_window_attention_workspace(lasad_ctx* ctx, const lasad_window_params* p);
+/* The gradient, from the forward's inputs and its o and lse, and d_o [B,T,Hq,d]: dq, dk, dv. */
+int lasad_window_attention_backward(lasad_ctx* ctx, const lasad_window_params* p, const void* q, const void* k,
+                                    const void* v, const void* o, const float* lse, const void* d_o,
+                                    const int32_t* lengths, void* dq, void* dk, void* dv, void* workspace,
+                                    void* cuda_stream);
+/*
+ * The same for one new token per sequence, q, o [B,Hq,d], k, v [B,Hk,d], against caches [B, sinks +
+ * window, Hk, d] that hold what it sees and nothing else: token i stands in slot i (i < sinks) or
+ * sinks + (i - sinks) mod window.  pos [B] int32 (device): the token's position; the slots that
+ * earlier tokens have filled must hold them.  The call writes k and v to the token's slot.  A
+ * negative position is a sequence that takes no part: its o is 0 and its cache is not touched.
+ */
+int64_t lasad_window_attention_step_workspace(lasad_ctx* ctx, const lasad_window_params* p);
+int lasad_window_attention_step(lasad_ctx* ctx, const lasad_window_params* p, const void* q, const void* k,
+                                const void* v, void* k_cache, void* v_cache, const int32_t* pos, void* o,
+                                void* workspace, void* cuda_stream);
+/* Puts the keys and values of a prefill, k, v [B,T,Hk,d] (tokens 0 to lengths[b] - 1, or T - 1), into
+ * such caches; slots that no token has reached are not written. */
+int lasad_window_cache_store(lasad_ctx* ctx, const lasad_window_params* p, const void* k, const void* v,
+                             const int32_t* lengths, void* k_cache, void* v_cache, void* cuda_stream);
 
 /* After the caller has synchronised the stream: 0, or LASAD_ERR_TIMEOUT if a kernel gave up a
  * bounded wait since the last query (the flag is cleared by the query).  Synchronous copy. */

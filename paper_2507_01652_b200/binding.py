@@ -13,25 +13,28 @@ import threading
 import torch
 
 from . import build as _build
+from . import mixers as _mixers
+from .marshal import (LASAD_BF16, LASAD_F32, _check_cuda, _dtype_code, _ptr, _raw_stream, _stream,  # noqa: F401
+                      _strides3, _strides_decode)
+from .mixers import rope_table  # noqa: F401
 
 LASAD_OK = 0
 LASAD_ERR_INVALID_ARG = -1
 LASAD_ERR_UNSUPPORTED = -2
 LASAD_ERR_CUDA = -3
 LASAD_ERR_TIMEOUT = -4
-LASAD_F32 = 0
-LASAD_BF16 = 1
 LASAD_OPT_PREFILL_IMPL = 0
 LASAD_OPT_PREFILL_CHUNK = 1
 LASAD_OPT_DECODE_TPU = 2
 LASAD_OPT_WAIT_LIMIT = 3
+LASAD_OPT_WINDOW_IMPL = 4
 
 EXPORTS = (
     "lasad_create", "lasad_destroy", "lasad_set_option", "lasad_reserve", "lasad_forward", "lasad_forward_host", "lasad_forward_static",
     "lasad_decode_step", "lasad_decode_step_pos", "lasad_forward_gated", "lasad_decode_step_gated",
     "lasad_forward_fused", "lasad_decode_step_fused",
     "lasad_last_device_status", "lasad_last_cuda_error", "lasad_launch_count", "lasad_strerror",
-)
+) + tuple(_mixers.PROTOTYPES)
 
 
 class LasadParams(ctypes.Structure):
@@ -101,35 +104,11 @@ def load_library() -> ctypes.CDLL:
         lib.lasad_launch_count.argtypes = [vp]
         lib.lasad_strerror.restype = ctypes.c_char_p
         lib.lasad_strerror.argtypes = [i32]
+        for name, (restype, argtypes) in _mixers.PROTOTYPES.items():
+            getattr(lib, name).restype = restype
+            getattr(lib, name).argtypes = argtypes
         _lib = lib
         return lib
-
-
-def _dtype_code(t: torch.Tensor) -> int:
-    if t.dtype == torch.float32:
-        return LASAD_F32
-    if t.dtype == torch.bfloat16:
-        return LASAD_BF16
-    raise TypeError(f"q, k, v, o must be float32 or bfloat16, got {t.dtype}")
-
-
-def _ptr(t):
-    # (an int is accepted where the prototype says c_void_p; None is a null pointer)
-    return None if t is None else t.data_ptr()
-
-
-try:
-    _raw_stream = torch._C._cuda_getCurrentRawStream     # the current stream's handle without a Stream object
-except AttributeError:       # pragma: no cover - older torch
-    _raw_stream = None
-
-
-def _stream(device, stream):
-    if stream is not None:
-        return stream
-    if _raw_stream is not None:
-        return _raw_stream(device.index if device.index is not None else torch.cuda.current_device())
-    return torch.cuda.current_stream(device).cuda_stream
 
 
 _params_cache = {}
@@ -160,26 +139,7 @@ def _params(kind, q, k, v, o, grid_w, prefix_len, t0, scale):
     return p
 
 
-def _check_cuda(*ts):
-    for t in ts:
-        if t is not None and not t.is_cuda:
-            raise ValueError("all tensors must be CUDA tensors (there is no CPU path)")
-
-
-def _strides3(t: torch.Tensor):
-    """Element strides of (batch, token, head) for a [B,T,H,d] view with contiguous channels."""
-    if t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1):
-        raise ValueError("expected [B,T,H,d] with contiguous channels")
-    return (ctypes.c_int64 * 3)(t.stride(0), t.stride(1), t.stride(2))
-
-
-def _strides_decode(t: torch.Tensor):
-    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
-        raise ValueError("expected [B,H,d] with contiguous channels")
-    return (ctypes.c_int64 * 3)(t.stride(0), 0, t.stride(1))
-
-
-class Lasad:
+class Lasad(_mixers.Mixers):
     """A ``lasad_ctx`` bound to one CUDA device."""
 
     def __init__(self, device: int | None = None):

@@ -162,6 +162,13 @@ int window_args(lasad_ctx* ctx, const lasad_window_params* p, int what, lasad::W
     return LASAD_OK;
 }
 
+// 1: CUDA cores, 2: tensor cores (LASAD_OPT_WINDOW_IMPL)
+int window_impl(const lasad_ctx* ctx, const lasad::WindowArgs& a)
+{
+    if (ctx->opt_window_impl == 0) return a.bf16 ? 2 : 1;
+    return ctx->opt_window_impl == 2 && !a.bf16 ? LASAD_ERR_UNSUPPORTED : ctx->opt_window_impl;
+}
+
 }  // namespace
 
 extern "C" {
@@ -264,7 +271,10 @@ int lasad_window_attention(lasad_ctx* ctx, const lasad_window_params* p, const v
     if (rc != LASAD_OK) return rc;
     if (!q || !k || !v || !o || !all16({q, k, v, o}) || !aligned(lengths, 4) || !aligned(lse, 4)) return LASAD_ERR_INVALID_ARG;
     a.q = q, a.k = k, a.v = v, a.o = o, a.lse = lse, a.lengths = lengths;
-    return launched(ctx, lasad::launch_window_forward_simt(a, static_cast<cudaStream_t>(cuda_stream)), 1);
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const int impl = window_impl(ctx, a);
+    if (impl < 0) return impl;
+    return launched(ctx, impl == 2 ? lasad::launch_window_forward_tc(a, st) : lasad::launch_window_forward_simt(a, st), 1);
 }
 
 int64_t lasad_window_attention_workspace(lasad_ctx* ctx, const lasad_window_params* p)

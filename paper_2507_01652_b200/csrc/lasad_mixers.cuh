@@ -156,6 +156,7 @@ __host__ __device__ inline size_t window_delta_floats(const WindowArgs& a) { ret
 size_t window_workspace_bytes(const WindowArgs& a);
 cudaError_t launch_window_prep(const WindowArgs& a, cudaStream_t st);
 cudaError_t launch_window_forward_tc(const WindowArgs& a, cudaStream_t st);      // bf16
+cudaError_t launch_window_backward_tc(const WindowArgs& a, cudaStream_t st);     // two launches, behind launch_window_prep
 cudaError_t launch_window_forward_simt(const WindowArgs& a, cudaStream_t st);
 cudaError_t launch_window_backward_simt(const WindowArgs& a, cudaStream_t st);   // two launches, behind launch_window_prep
 // One token against the ring cache.  splits: CTAs along the slots (window_step_splits).

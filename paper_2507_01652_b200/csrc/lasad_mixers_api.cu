@@ -298,8 +298,10 @@ int lasad_window_attention_backward(lasad_ctx* ctx, const lasad_window_params* p
     a.q = q, a.k = k, a.v = v, a.o = const_cast<void*>(o), a.lse = const_cast<float*>(lse), a.dout = d_o;
     a.lengths = lengths, a.dq = dq, a.dk = dk, a.dv = dv, a.ws = static_cast<float*>(workspace);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const int impl = window_impl(ctx, a);
+    if (impl < 0) return impl;
     cudaError_t e = lasad::launch_window_prep(a, st);
-    if (e == cudaSuccess) e = lasad::launch_window_backward_simt(a, st);
+    if (e == cudaSuccess) e = impl == 2 ? lasad::launch_window_backward_tc(a, st) : lasad::launch_window_backward_simt(a, st);
     return launched(ctx, e, 3);
 }
 

@@ -166,7 +166,7 @@ window_forward_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
         constexpr uint32_t idesc_pv = make_idesc(128, 64, 0, 1);  // P (tmem) x V (MN-major)
         auto issue_s = [&](int j) {
             const int s = j % kStages;
-            if (!mbar_wait(&sm.k_full[s], (j / kStages) & 1, limit, abort_flag, p.status)) return false;
+            if (!warp_wait(&sm.k_full[s], (j / kStages) & 1, limit, abort_flag, p.status)) return false;
             tc_fence_after();
             if (elect_one()) {
                 const uint32_t idesc = make_idesc(128, 32 * blocks_of(j), 0, 0) | minus;
@@ -179,14 +179,14 @@ window_forward_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
             __syncwarp();
             return true;
         };
-        bool ok = n > 0 && mbar_wait(&sm.q_full, 0, limit, abort_flag, p.status) && issue_s(0);
+        bool ok = n > 0 && warp_wait(&sm.q_full, 0, limit, abort_flag, p.status) && issue_s(0);
         for (int j = 0; ok && j < n; ++j) {
             const int s = j % kStages;
             if (j + 1 < n) {
-                if (!mbar_wait(&sm.s_free, j & 1, limit, abort_flag, p.status) || !issue_s(j + 1)) break;
+                if (!warp_wait(&sm.s_free, j & 1, limit, abort_flag, p.status) || !issue_s(j + 1)) break;
             }
-            if (!mbar_wait(&sm.v_full[s], (j / kStages) & 1, limit, abort_flag, p.status)) break;
-            if (!mbar_wait(&sm.p_ready, j & 1, limit, abort_flag, p.status)) break;
+            if (!warp_wait(&sm.v_full[s], (j / kStages) & 1, limit, abort_flag, p.status)) break;
+            if (!warp_wait(&sm.p_ready, j & 1, limit, abort_flag, p.status)) break;
             tc_fence_after();
             if (elect_one()) {
                 const uint64_t dv = s ? dv1 : dv0;
@@ -221,7 +221,7 @@ window_forward_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
                 const bool all = s1 <= tw0 && s1 < len && (tw1 - s0 < p.window || s1 < p.sinks);
                 vis[c] = !any ? 0 : all ? 2 : 1;
             }
-            if (!(ok = mbar_wait(&sm.s_full, j & 1, limit, abort_flag, p.status))) break;
+            if (!(ok = warp_wait(&sm.s_full, j & 1, limit, abort_flag, p.status))) break;
             tc_fence_after();
             uint32_t sv[4][32];
 #pragma unroll
@@ -245,7 +245,7 @@ window_forward_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
             }
             top *= p.scale2;
             // P of the tile before has been used, and O is complete up to it
-            if (j > 0 && !(ok = mbar_wait(&sm.o_done, (j - 1) & 1, limit, abort_flag, p.status))) break;
+            if (j > 0 && !(ok = warp_wait(&sm.o_done, (j - 1) & 1, limit, abort_flag, p.status))) break;
             tc_fence_after();
             const bool grow = top > m + 8.0f || (m == -INFINITY && top > m);
             if (j == 0) {
@@ -289,7 +289,7 @@ window_forward_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
             }
             // values past the sequence's end do not count, whatever they are
             if (len < p.T && k0 + kRows > len) {
-                if (!(ok = mbar_wait(&sm.v_full[j % kStages], (j / kStages) & 1, limit, abort_flag, p.status))) break;
+                if (!(ok = warp_wait(&sm.v_full[j % kStages], (j / kStages) & 1, limit, abort_flag, p.status))) break;
                 if (k0 + row >= len) zero_row(sm.v[j % kStages] + row * 128);
                 fence_proxy_async();
             }
@@ -297,7 +297,7 @@ window_forward_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
             tc_fence_before();
             mbar_arrive(&sm.p_ready);
         }
-        if (ok && n > 0) ok = mbar_wait(&sm.o_done, (n - 1) & 1, limit, abort_flag, p.status);
+        if (ok && n > 0) ok = warp_wait(&sm.o_done, (n - 1) & 1, limit, abort_flag, p.status);
         if (ok) {
             tc_fence_after();
             const float l = l0 + l1;

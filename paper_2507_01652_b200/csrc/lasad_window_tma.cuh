@@ -43,6 +43,12 @@ __device__ __forceinline__ uint32_t seen_bits(int t, int s0, int window, int sin
     return bit_range(t - window + 1 - s0, last) | bit_range(0, min(last, sinks - 1 - s0));
 }
 
+// mbar_wait of a whole warp: every lane goes on, or none does, so that what follows may need all of them.
+__device__ __forceinline__ bool warp_wait(void* bar, unsigned parity, unsigned limit, volatile int* abort_flag, int* status)
+{
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, limit, abort_flag, status));
+}
+
 // Zeroes one 128-byte row of a tile.
 __device__ __forceinline__ void zero_row(unsigned char* row)
 {

@@ -77,10 +77,10 @@ struct ScanArgs {
     float* dh_in;          // [B,C] or null
     const int* pos;        // step only: [B] or null (t0 for all)
     // how the work is cut (scan_plan)
-    int tile, segs, seg_chunks;
-    float* ws;             // [B, segs, 2, C] when segs > 1
+    int whole, segs, seg_chunks;
+    float* ws;             // the segments' summaries when segs > 1
 };
-void scan_plan(ScanArgs& a, int sms);
+void scan_plan(ScanArgs& a, bool backward, int sms);
 size_t scan_workspace_bytes(const ScanArgs& a);
 int scan_launches(const ScanArgs& a);
 cudaError_t launch_scan_forward(const ScanArgs& a, cudaStream_t st);

@@ -57,7 +57,7 @@ int scan_args(lasad_ctx* ctx, const lasad_scan_params* p, bool step, bool backwa
         if (s[0] < 0 || (s[0] == 0 && p->B > 1)) return LASAD_ERR_INVALID_ARG;
         if (!step && (s[1] < 0 || (s[1] < p->C && p->T > 1))) return LASAD_ERR_INVALID_ARG;
     }
-    if (p->B > 65535 || (int64_t)p->B * p->C > 0x7fffffffLL) return LASAD_ERR_UNSUPPORTED;
+    if (p->B > 65535 || (int64_t)p->B * p->C > 0x7fffffffLL || (!step && p->T > (1 << 30))) return LASAD_ERR_UNSUPPORTED;
     if (on_device(ctx) != LASAD_OK) return LASAD_ERR_INVALID_ARG;
     a.B = p->B, a.T = step ? 1 : p->T, a.C = p->C;
     a.grid_w = p->grid_w, a.prefix_len = p->prefix_len, a.t0 = p->t0;
@@ -67,7 +67,7 @@ int scan_args(lasad_ctx* ctx, const lasad_scan_params* p, bool step, bool backwa
         a.xs[i] = p->x_stride[i], a.gs[i] = p->gate_stride[i], a.ys[i] = p->y_stride[i];
         if (backward) a.dxs[i] = p->dx_stride[i], a.dgs[i] = p->dgate_stride[i];
     }
-    if (!step) lasad::scan_plan(a, ctx->sm_count);
+    if (!step) lasad::scan_plan(a, backward, ctx->sm_count);
     return LASAD_OK;
 }
 bool scan_aligned(const lasad::ScanArgs& a, std::initializer_list<const void*> data, std::initializer_list<const void*> states)
@@ -177,7 +177,10 @@ int64_t lasad_scan_workspace(lasad_ctx* ctx, const lasad_scan_params* p)
 {
     lasad::ScanArgs a{};
     const int rc = scan_args(ctx, p, false, false, a);
-    return rc != LASAD_OK ? rc : (int64_t)lasad::scan_workspace_bytes(a);
+    if (rc != LASAD_OK) return rc;
+    const size_t forward = lasad::scan_workspace_bytes(a);
+    lasad::scan_plan(a, true, ctx->sm_count);
+    return (int64_t)std::max(forward, lasad::scan_workspace_bytes(a));
 }
 
 int lasad_scan_forward(lasad_ctx* ctx, const lasad_scan_params* p, const void* x, const void* gate, const float* h_in,

@@ -21,318 +21,537 @@
 // composition of those before it.  No CTA ever waits for another one.
 #include "lasad_mixers.cuh"
 #include "lasad_tc_ptx.cuh"
+#include "lasad_tc_tma.cuh"
 
 namespace lasad {
 namespace {
 
 constexpr int kSlots = 16, kTok = kScanChunk / kSlots;
 
-// lambda = sigmoid(z) and 1 - lambda, each to full relative precision: the smaller of the two is
-// e^-|z| / (1 + e^-|z|), never a difference.  (No clamp: infinities and NaN come out as they should.)
-__device__ __forceinline__ void gate_of(float z, bool logits, float& lam, float& rest)
-{
-    if (logits) {
-        const float t = tcx::ex2_approx(fabsf(z) * -1.4426950408889634f);
-        const float big = __fdividef(1.0f, 1.0f + t), small = t * big;
-        lam = z < 0.0f ? small : big;
-        rest = z < 0.0f ? big : small;
-    } else {
-        lam = z;
-        rest = 1.0f - z;
+// VEC neighbouring channels as one number: pairs use the packed fp32 arithmetic of sm_100, which
+// halves the instructions (the kernels are near the issue rate at full memory speed).
+template <int VEC> struct num;
+template <> struct num<1> {
+    float v;
+    static __device__ __forceinline__ num all(float x) { return {x}; }
+    __device__ __forceinline__ float get(int) const { return v; }
+    __device__ __forceinline__ void set(int, float x) { v = x; }
+};
+template <> struct num<2> {
+    unsigned long long v;
+    static __device__ __forceinline__ num of(float a, float b)
+    {
+        num r;
+        asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+        return r;
     }
+    static __device__ __forceinline__ num all(float x) { return of(x, x); }
+    __device__ __forceinline__ float get(int i) const
+    {
+        float a, b;
+        asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
+        return i ? b : a;
+    }
+    __device__ __forceinline__ void set(int i, float x) { *this = i ? of(get(0), x) : of(x, get(1)); }
+};
+__device__ __forceinline__ num<1> operator*(num<1> a, num<1> b) { return {a.v * b.v}; }
+__device__ __forceinline__ num<1> operator+(num<1> a, num<1> b) { return {a.v + b.v}; }
+__device__ __forceinline__ num<1> fma(num<1> a, num<1> b, num<1> c) { return {fmaf(a.v, b.v, c.v)}; }
+__device__ __forceinline__ num<2> operator*(num<2> a, num<2> b)
+{
+    num<2> r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ num<2> operator+(num<2> a, num<2> b)
+{
+    num<2> r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ num<2> fma(num<2> a, num<2> b, num<2> c)
+{
+    num<2> r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
 }
 
-// VEC neighbouring channels in one access (VEC = 2 needs pairs that are aligned to a pair)
+// VEC channels in memory (VEC = 2 needs pairs that are aligned to a pair)
 template <typename T, int VEC> struct pack;
 template <> struct pack<__nv_bfloat16, 2> {
     typedef uint32_t raw;
-    static __device__ __forceinline__ void get(raw r, float (&v)[2]) { v[0] = tcx::bf16_lo(r); v[1] = tcx::bf16_hi(r); }
-    static __device__ __forceinline__ raw put(const float (&v)[2]) { return tcx::pack_bf16(v[0], v[1]); }
+    static __device__ __forceinline__ raw all(float x) { return tcx::pack_bf16(x, x); }
+    static __device__ __forceinline__ num<2> get(raw r) { return num<2>::of(tcx::bf16_lo(r), tcx::bf16_hi(r)); }
+    static __device__ __forceinline__ raw put(num<2> v) { return tcx::pack_bf16(v.get(0), v.get(1)); }
 };
 template <> struct pack<__nv_bfloat16, 1> {
     typedef unsigned short raw;
-    static __device__ __forceinline__ void get(raw r, float (&v)[1]) { v[0] = __uint_as_float((uint32_t)r << 16); }
-    static __device__ __forceinline__ raw put(const float (&v)[1]) { return __bfloat16_as_ushort(__float2bfloat16_rn(v[0])); }
+    static __device__ __forceinline__ raw all(float x) { return __bfloat16_as_ushort(__float2bfloat16_rn(x)); }
+    static __device__ __forceinline__ num<1> get(raw r) { return {__uint_as_float((uint32_t)r << 16)}; }
+    static __device__ __forceinline__ raw put(num<1> v) { return __bfloat16_as_ushort(__float2bfloat16_rn(v.v)); }
 };
 template <> struct pack<float, 2> {
     typedef float2 raw;
-    static __device__ __forceinline__ void get(raw r, float (&v)[2]) { v[0] = r.x; v[1] = r.y; }
-    static __device__ __forceinline__ raw put(const float (&v)[2]) { return make_float2(v[0], v[1]); }
+    static __device__ __forceinline__ raw all(float x) { return make_float2(x, x); }
+    static __device__ __forceinline__ num<2> get(raw r) { return num<2>::of(r.x, r.y); }
+    static __device__ __forceinline__ raw put(num<2> v) { return make_float2(v.get(0), v.get(1)); }
 };
 template <> struct pack<float, 1> {
     typedef float raw;
-    static __device__ __forceinline__ void get(raw r, float (&v)[1]) { v[0] = r; }
-    static __device__ __forceinline__ raw put(const float (&v)[1]) { return v[0]; }
+    static __device__ __forceinline__ raw all(float x) { return x; }
+    static __device__ __forceinline__ num<1> get(raw r) { return {r}; }
+    static __device__ __forceinline__ raw put(num<1> v) { return v.v; }
+};
+
+// VEC floats of a state
+template <int VEC>
+__device__ __forceinline__ num<VEC> load_state(const float* p)
+{
+    num<VEC> r = num<VEC>::all(0.0f);
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) r.set(v, p[v]);
+    return r;
+}
+template <int VEC>
+__device__ __forceinline__ void store_state(float* p, num<VEC> x)
+{
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) p[v] = x.get(v);
+}
+
+// lambda = sigmoid(z) = 1 / (1 + t) and 1 - lambda = t / (1 + t) with t = e^-z, each to full
+// relative precision.  The exponent ends at 126, where lambda is 2^-126 and the products stay finite;
+// a NaN passes through.
+template <bool LOGITS, int VEC>
+__device__ __forceinline__ void gate_of(num<VEC> z, num<VEC>& lam, num<VEC>& rest)
+{
+    if (LOGITS) {
+        const num<VEC> e = z * num<VEC>::all(-1.4426950408889634f);
+        num<VEC> t = e;
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+            float x;
+            asm("min.NaN.f32 %0, %1, 0f42fc0000;" : "=f"(x) : "f"(e.get(v)));
+            t.set(v, tcx::ex2_approx(x));
+        }
+        const num<VEC> s = t + num<VEC>::all(1.0f);
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+            float x;
+            asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(x) : "f"(s.get(v)));
+            lam.set(v, x);
+        }
+        rest = t * lam;
+    } else {
+        lam = z;
+        rest = fma(z, num<VEC>::all(-1.0f), num<VEC>::all(1.0f));
+    }
+}
+
+// Which of a slot's kTok tokens end a grid row, for slots that are visited a chunk further on, or
+// back, each time.
+struct RowEnds {
+    long long j;         // grid index of the slot's first token (negative before the grid)
+    int w, col, step;    // col = j mod w where j >= 0
+    __device__ __forceinline__ RowEnds(long long i, int grid_w, int prefix_len) : j(i - prefix_len), w(grid_w), col(0), step(0)
+    {
+        if (w > 0) {
+            step = kScanChunk % w;
+            if (j >= 0) col = (int)(j % w);
+        }
+    }
+    __device__ __forceinline__ unsigned mask() const
+    {
+        if (w <= 0) return 0u;
+        unsigned m = 0;
+        const long long first = j >= 0 ? w - 1 - col : w - 1 - j;
+        for (int e = first < kTok ? (int)first : kTok; e < kTok; e += w) m |= 1u << e;
+        return m;
+    }
+    __device__ __forceinline__ void forward()
+    {
+        const bool on = j >= 0;
+        j += kScanChunk;
+        if (w <= 0) return;
+        if (on) {
+            col += step;
+            if (col >= w) col -= w;
+        } else if (j >= 0) {
+            col = (int)(j % w);
+        }
+    }
+    __device__ __forceinline__ void back()
+    {
+        j -= kScanChunk;
+        if (w <= 0 || j < 0) return;
+        col -= step;
+        if (col < 0) col += w;
+    }
+};
+
+// What a CTA has to do: chunks first .. end - 1 of the channels from c on, of batch element b.  The first
+// a.whole tiles are whole sequences, the others are cut into a.segs segments (see scan_plan).
+struct Work {
+    int b, c, seg, segs, first, end, cut, cuts, width;
+    // summary: the first segment that a summary is made of, or -1 (not a summary: every tile's work)
+    __device__ __forceinline__ Work(const ScanArgs& a, int summary, int chunks, int w) : width(w)
+    {
+        const int per = (a.C + w - 1) / w;
+        int at = blockIdx.x, tile;
+        cuts = a.B * per - a.whole;
+        if (summary < 0 && at < a.whole) {
+            tile = at;
+            seg = cut = 0;
+            segs = 1;
+        } else {
+            if (summary < 0) at -= a.whole;
+            seg = at / cuts;
+            cut = at - seg * cuts;
+            seg += max(summary, 0);
+            tile = a.whole + cut;
+            segs = a.segs;
+        }
+        b = tile / per;
+        c = (tile - b * per) * w;
+        first = segs == 1 ? 0 : seg * a.seg_chunks;
+        end = segs == 1 ? chunks : min(first + a.seg_chunks, chunks);
+    }
+    // (A, H) or (A, Q) of segment s of this CTA's tile: 2 x width floats
+    __device__ __forceinline__ float* span(const ScanArgs& a, int s) const
+    {
+        return a.ws + ((long long)s * cuts + cut) * 2 * width;
+    }
+};
+
+// How a tile of NA tensors comes into shared memory: rows of the tile's channels, kTok rows to a slot,
+// and 64 bytes between slots, so that the two slots of a warp (16 lanes of pairs) use different
+// banks.  A warp copies the rows of its own slots, so a chunk's arrival is a matter of the warp alone.
+// WIDE: 16-byte asynchronous copies, one chunk ahead (pointers, strides and C in whole 16 bytes).
+// Otherwise every lane fetches its own channels; right for any alignment, and slower.
+template <typename T, int VEC, int LC, int NA, bool WIDE>
+struct Stage {
+    typedef typename pack<T, VEC>::raw raw;
+    static constexpr int kRow = LC * VEC * (int)sizeof(T), kSlot = kTok * kRow + 64, kArray = kSlots * kSlot;
+    static constexpr int kBytes = 2 * NA * kArray;                 // two chunks
+    static constexpr int kPieces = kRow / 16, kRows = 32 / LC * kTok, kCopies = kRows * kPieces / 32;
+    unsigned char* mem;
+    const T* src[NA];        // WIDE: the lane's first piece of the warp's first row; else the lane's channels there
+    long long stride[NA];
+    int row, piece;          // WIDE: of the lane's first copy
+    bool in;
+    __device__ __forceinline__ Stage(unsigned char* m, int lane32, int warp) : mem(m)
+    {
+        row = lane32 / kPieces;
+        piece = lane32 % kPieces;
+        mem += warp * (32 / LC) * kSlot;
+    }
+    // base: the CTA's first channel at the warp's first token of the first chunk
+    __device__ __forceinline__ void tensor(int n, const void* base, long long str, int c_tile, int C)
+    {
+        const int lane = threadIdx.x % LC, sub = (threadIdx.x & 31) / LC;
+        stride[n] = str;
+        if (WIDE) {
+            const int c = piece * (16 / (int)sizeof(T));
+            src[n] = static_cast<const T*>(base) + row * str + c;
+            in = c_tile + c < C;
+        } else {
+            src[n] = static_cast<const T*>(base) + sub * kTok * str + lane * VEC;
+            in = c_tile + lane * VEC < C;
+        }
+    }
+    // rows: tokens from the warp's first one to the end of the sequence
+    __device__ __forceinline__ void fetch(int buf, int rows)
+    {
+#pragma unroll
+        for (int n = 0; n < NA; ++n) {
+            unsigned char* to = mem + (buf * NA + n) * kArray;
+            if (WIDE) {
+#pragma unroll
+                for (int k = 0; k < kCopies; ++k) {
+                    const int r = row + k * (32 / kPieces);
+                    const bool live = in && r < rows;
+                    const uint32_t dst = tcx::smem_u32(to + (r / kTok) * kSlot + (r % kTok) * kRow + piece * 16);
+                    const T* from = live ? src[n] + (long long)(k * (32 / kPieces)) * stride[n] : src[n];
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(from), "r"(live ? 16 : 0) : "memory");
+                }
+            } else {
+                const int lane = threadIdx.x % LC, sub = (threadIdx.x & 31) / LC;
+#pragma unroll
+                for (int t = 0; t < kTok; ++t)
+                    if (in && sub * kTok + t < rows)
+                        reinterpret_cast<raw*>(to + sub * kSlot + t * kRow)[lane] = *reinterpret_cast<const raw*>(src[n] + t * stride[n]);
+            }
+        }
+        if (WIDE) asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    __device__ __forceinline__ void move(int chunks)
+    {
+#pragma unroll
+        for (int n = 0; n < NA; ++n) src[n] += chunks * kScanChunk * stride[n];
+    }
+    __device__ __forceinline__ void landed(bool last)
+    {
+        if (WIDE) {
+            if (last) asm volatile("cp.async.wait_group 0;" ::: "memory");
+            else asm volatile("cp.async.wait_group 1;" ::: "memory");
+        }
+        __syncwarp();
+    }
+    // the thread's channels of token t of its slot
+    __device__ __forceinline__ raw get(int buf, int n, int t) const
+    {
+        const int lane = threadIdx.x % LC, sub = (threadIdx.x & 31) / LC;
+        return reinterpret_cast<const raw*>(mem + (buf * NA + n) * kArray + sub * kSlot + t * kRow)[lane];
+    }
 };
 
 // LC lanes of VEC channels make a tile; a CTA has LC * kSlots threads.
-template <typename T, int VEC, int LC, bool LOGITS, bool SUMMARY>
-__global__ void __launch_bounds__(LC * kSlots) scan_forward_kernel(const ScanArgs a)
+// SUMMARY: only (A, H) of a whole segment.
+template <typename T, int VEC, int LC, bool WIDE, bool LOGITS, bool TIED, bool SUMMARY>
+__global__ void __launch_bounds__(LC * kSlots, LC == 16 ? 3 : 1) scan_forward_kernel(const ScanArgs a)
 {
     typedef pack<T, VEC> P;
     typedef typename P::raw raw;
-    __shared__ float2 pair[2][kSlots][LC * VEC];   // (A, H) of every slot, two chunks in turn
-    __shared__ float next[2][LC * VEC];            // h after the chunk
-    const int lane = threadIdx.x % LC, slot = threadIdx.x / LC;
-    const int tiles = (a.C + LC * VEC - 1) / (LC * VEC);
-    const int b = blockIdx.x / tiles, c0 = (blockIdx.x - b * tiles) * LC * VEC + lane * VEC;
-    const int seg = blockIdx.y, chunks = (a.T + kScanChunk - 1) / kScanChunk;
-    const int first = seg * a.seg_chunks, end = min(first + a.seg_chunks, chunks);
+    typedef num<VEC> N;
+    struct Span { N A, H; };
+    extern __shared__ __align__(16) unsigned char mem[];
+    __shared__ Span span[2][kSlots][LC];           // of every slot, two chunks in turn
+    __shared__ N next[2][LC];                      // h after the chunk
+    const int lane = threadIdx.x % LC, slot = threadIdx.x / LC, warp = threadIdx.x >> 5;
+    const int chunks = (a.T + kScanChunk - 1) / kScanChunk;
+    const Work wk(a, SUMMARY ? 0 : -1, chunks, LC * VEC);
+    const int b = wk.b, tile0 = wk.c, c0 = tile0 + lane * VEC, first = wk.first, end = wk.end;
     const bool in = c0 < a.C;                      // (VEC = 2 only where C is even)
-    const T* x = static_cast<const T*>(a.x) + b * a.xs[0] + c0;
-    const T* z = static_cast<const T*>(a.gate) + b * a.gs[0] + c0;
-    T* y = static_cast<T*>(a.y) + b * a.ys[0] + c0;
+    const int w0 = first * kScanChunk + warp * (32 / LC) * kTok, t0 = first * kScanChunk + slot * kTok;
+    Stage<T, VEC, LC, 2, WIDE> st(mem, threadIdx.x & 31, warp);
+    st.tensor(0, static_cast<const T*>(a.x) + b * a.xs[0] + tile0 + w0 * a.xs[1], a.xs[1], tile0, a.C);
+    st.tensor(1, static_cast<const T*>(a.gate) + b * a.gs[0] + tile0 + w0 * a.gs[1], a.gs[1], tile0, a.C);
+    T* y = static_cast<T*>(a.y) + b * a.ys[0] + c0 + t0 * a.ys[1];
+    const long long state = (long long)b * a.C + c0;
+    RowEnds rows(a.t0 + t0, a.grid_w, a.prefix_len);
+    int rest_rows = a.T - w0, left = a.T - t0;     // tokens from the warp's, the slot's first one to the end
     pdl_wait();
-
-    raw rx[kTok], rz[kTok];
-    auto load = [&](int chunk) {
-        const int t0 = chunk * kScanChunk + slot * kTok;
-#pragma unroll
-        for (int t = 0; t < kTok; ++t)
-            if (in && chunk < end && t0 + t < a.T) {
-                rx[t] = *reinterpret_cast<const raw*>(x + (long long)(t0 + t) * a.xs[1]);
-                rz[t] = *reinterpret_cast<const raw*>(z + (long long)(t0 + t) * a.gs[1]);
-            }
-    };
-    load(first);
+    st.fetch(first & 1, rest_rows);
     // the state at the segment's first token: h_in through the segments before it
-    float h0[VEC], total[VEC];
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) {
-        h0[v] = !SUMMARY && a.h_in && in ? a.h_in[(long long)b * a.C + c0 + v] : 0.0f;
-        total[v] = 1.0f;
-    }
+    N h0 = N::all(0.0f), total = N::all(1.0f);
     if (!SUMMARY && in) {
-        const float* w = a.ws + (long long)b * a.segs * 2 * a.C + c0;
+        if (a.h_in) h0 = load_state<VEC>(a.h_in + state);
 #pragma unroll 4
-        for (int s = 0; s < seg; ++s, w += 2 * a.C)
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) h0[v] = fmaf(w[v], h0[v], w[a.C + v]);
+        for (int s = 0; s < wk.seg; ++s) {
+            const float* w = wk.span(a, s) + lane * VEC;
+            h0 = fma(load_state<VEC>(w), h0, load_state<VEC>(w + LC * VEC));
+        }
     }
     for (int chunk = first; chunk < end; ++chunk) {
-        const int buf = chunk & 1, t0 = chunk * kScanChunk + slot * kTok;
-        float ca[kTok][VEC], cb[kTok][VEC], A[VEC], H[VEC];
-        RowWalk row(a.t0 + t0, a.grid_w, a.prefix_len);
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) A[v] = 1.0f, H[v] = 0.0f;
+        const int buf = chunk & 1;
+        // the next chunk comes in under this one's arithmetic (its buffer was read before the last barrier)
+        if (chunk + 1 < end) {
+            st.move(1);
+            st.fetch(buf ^ 1, rest_rows - kScanChunk);
+        }
+        st.landed(chunk + 1 == end);
+        N ca[kTok], cb[kTok];
 #pragma unroll
         for (int t = 0; t < kTok; ++t) {
-            const bool ends = row.step(), live = in && t0 + t < a.T;
-            float xv[VEC], zv[VEC];
-            P::get(rx[t], xv);
-            P::get(rz[t], zv);
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) {
-                float lam, rest;
-                gate_of(zv[v], LOGITS, lam, rest);
-                ca[t][v] = ends || !live ? 1.0f : lam;
-                cb[t][v] = !live ? 0.0f : a.tied ? rest * xv[v] : xv[v];
-                A[v] *= ca[t][v];
-                H[v] = fmaf(ca[t][v], H[v], cb[t][v]);
-            }
+            N rest;
+            const N xv = P::get(st.get(buf, 0, t));
+            gate_of<LOGITS>(P::get(st.get(buf, 1, t)), ca[t], rest);
+            cb[t] = TIED ? rest * xv : xv;
         }
-        load(chunk + 1);
+        const unsigned ends = rows.mask();
+        if (ends)
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) pair[buf][slot][lane * VEC + v] = make_float2(A[v], H[v]);
+            for (int t = 0; t < kTok; ++t)
+                if ((ends >> t) & 1u) ca[t] = N::all(1.0f);
+        if (left < kTok)                           // a token past the end changes nothing
+#pragma unroll
+            for (int t = 0; t < kTok; ++t)
+                if (t >= left) ca[t] = N::all(1.0f), cb[t] = N::all(0.0f);
+        N A = ca[0], H = cb[0];
+#pragma unroll
+        for (int t = 1; t < kTok; ++t) {
+            A = A * ca[t];
+            H = fma(ca[t], H, cb[t]);
+        }
+        span[buf][slot][lane] = {A, H};
         __syncthreads();
         // h before this slot (the chunk's own start came through `next` at the same barrier)
-        float h[VEC];
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) h[v] = chunk == first ? h0[v] : next[buf][lane * VEC + v];
+        N h = chunk == first ? h0 : next[buf][lane];
         if (!SUMMARY && slot == 0 && a.saved && in)
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) a.saved[((long long)b * chunks + chunk) * a.C + c0 + v] = h[v];
-        for (int s = 0; s < slot; ++s)
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) {
-                const float2 m = pair[buf][s][lane * VEC + v];
-                h[v] = fmaf(m.x, h[v], m.y);
-                if (SUMMARY && slot == kSlots - 1) total[v] *= m.x;
-            }
-        if (slot == kSlots - 1)
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) {
-                const float after = fmaf(A[v], h[v], H[v]);
-                if (SUMMARY) total[v] *= A[v];
-                next[buf ^ 1][lane * VEC + v] = after;
-                if (chunk == end - 1 && in) {
-                    if (SUMMARY) {
-                        float* w = a.ws + ((long long)b * a.segs + seg) * 2 * a.C + c0 + v;
-                        w[0] = total[v];
-                        w[a.C] = after;
-                    } else if (end == chunks && a.h_out) {
-                        a.h_out[(long long)b * a.C + c0 + v] = after;
-                    }
+            store_state<VEC>(a.saved + ((long long)b * chunks + chunk) * a.C + c0, h);
+#pragma unroll 5
+        for (int s = 0; s < slot; ++s) {
+            const Span m = span[buf][s][lane];
+            h = fma(m.A, h, m.H);
+            if (SUMMARY && slot == kSlots - 1) total = total * m.A;
+        }
+        if (slot == kSlots - 1) {
+            const N after = fma(A, h, H);
+            if (SUMMARY) total = total * A;
+            next[buf ^ 1][lane] = after;
+            if (chunk == end - 1 && in) {
+                if (SUMMARY) {
+                    float* w = wk.span(a, wk.seg) + lane * VEC;
+                    store_state<VEC>(w, total);
+                    store_state<VEC>(w + LC * VEC, after);
+                } else if (end == chunks && a.h_out) {
+                    store_state<VEC>(a.h_out + state, after);
                 }
             }
+        }
         if (!SUMMARY && in)
 #pragma unroll
             for (int t = 0; t < kTok; ++t) {
-                if (t0 + t < a.T) {
-#pragma unroll
-                    for (int v = 0; v < VEC; ++v) h[v] = fmaf(ca[t][v], h[v], cb[t][v]);
-                    *reinterpret_cast<raw*>(y + (long long)(t0 + t) * a.ys[1]) = P::put(h);
-                }
+                h = fma(ca[t], h, cb[t]);
+                if (t < left) *reinterpret_cast<raw*>(y + t * a.ys[1]) = P::put(h);
             }
+        y += kScanChunk * a.ys[1];
+        rest_rows -= kScanChunk;
+        left -= kScanChunk;
+        rows.forward();
     }
 }
 
 // The same walk from the end.  With u_t = a_t g_t the reversed recurrence u_t = a_t (u_{t+1} + dy_t)
 // has the forward's products A, so a slot's spans in both directions are (A, H) and (A, Q).
 // SUMMARY: only (A, Q) of a whole segment, from lambda and dy.
-template <typename T, int VEC, int LC, bool LOGITS, bool SUMMARY>
-__global__ void __launch_bounds__(LC * kSlots) scan_backward_kernel(const ScanArgs a)
+template <typename T, int VEC, int LC, bool WIDE, bool LOGITS, bool TIED, bool SUMMARY>
+__global__ void __launch_bounds__(LC * kSlots, LC != 16 ? 1 : sizeof(T) == 2 ? 2 : 1) scan_backward_kernel(const ScanArgs a)
 {
     typedef pack<T, VEC> P;
     typedef typename P::raw raw;
-    __shared__ float2 pair[2][kSlots][LC * VEC];   // (A, Q) of every slot
-    __shared__ float fwd[2][kSlots][LC * VEC];     // H of every slot
-    __shared__ float next[2][LC * VEC];            // u before the chunk
-    const int lane = threadIdx.x % LC, slot = threadIdx.x / LC;
-    const int tiles = (a.C + LC * VEC - 1) / (LC * VEC);
-    const int b = blockIdx.x / tiles, c0 = (blockIdx.x - b * tiles) * LC * VEC + lane * VEC;
+    typedef num<VEC> N;
+    struct Span { N A, X; };
+    extern __shared__ __align__(16) unsigned char mem[];
+    __shared__ Span back[2][kSlots][LC];           // (A, Q) of every slot
+    __shared__ N fwd[SUMMARY ? 1 : 2][kSlots][LC]; // H
+    __shared__ N next[2][LC];                      // u before the chunk
+    const int lane = threadIdx.x % LC, slot = threadIdx.x / LC, warp = threadIdx.x >> 5;
     const int chunks = (a.T + kScanChunk - 1) / kScanChunk;
-    const int seg = SUMMARY ? blockIdx.y + 1 : blockIdx.y;      // (nothing comes before segment 0: it needs no summary)
-    const int first = seg * a.seg_chunks, end = min(first + a.seg_chunks, chunks);
+    const Work wk(a, SUMMARY ? 1 : -1, chunks, LC * VEC);       // (nothing comes before segment 0: it needs no summary)
+    const int b = wk.b, tile0 = wk.c, c0 = tile0 + lane * VEC, first = wk.first, end = wk.end;
     const bool in = c0 < a.C;
-    const T* x = static_cast<const T*>(a.x) + b * a.xs[0] + c0;
-    const T* z = static_cast<const T*>(a.gate) + b * a.gs[0] + c0;
-    const T* dy = static_cast<const T*>(a.dy) + b * a.ys[0] + c0;
-    T* dx = static_cast<T*>(a.dx) + b * a.dxs[0] + c0;
-    T* dg = static_cast<T*>(a.dgate) + b * a.dgs[0] + c0;
+    const int w0 = (end - 1) * kScanChunk + warp * (32 / LC) * kTok, t0 = (end - 1) * kScanChunk + slot * kTok;
+    Stage<T, VEC, LC, SUMMARY ? 2 : 3, WIDE> st(mem, threadIdx.x & 31, warp);
+    st.tensor(0, static_cast<const T*>(a.gate) + b * a.gs[0] + tile0 + w0 * a.gs[1], a.gs[1], tile0, a.C);
+    st.tensor(1, static_cast<const T*>(a.dy) + b * a.ys[0] + tile0 + w0 * a.ys[1], a.ys[1], tile0, a.C);
+    if constexpr (!SUMMARY) st.tensor(2, static_cast<const T*>(a.x) + b * a.xs[0] + tile0 + w0 * a.xs[1], a.xs[1], tile0, a.C);
+    T* dx = static_cast<T*>(a.dx) + b * a.dxs[0] + c0 + t0 * a.dxs[1];
+    T* dg = static_cast<T*>(a.dgate) + b * a.dgs[0] + c0 + t0 * a.dgs[1];
+    const float* saved = a.saved + ((long long)b * chunks + end - 1) * a.C + c0;
+    const long long state = (long long)b * a.C + c0;
+    RowEnds rows(a.t0 + t0, a.grid_w, a.prefix_len);
+    int rest_rows = a.T - w0, left = a.T - t0;
     pdl_wait();
-
-    raw rx[kTok], rz[kTok], rd[kTok];
-    float hs[VEC];                                 // h before the chunk
-    auto load = [&](int chunk) {
-        const int t0 = chunk * kScanChunk + slot * kTok;
-#pragma unroll
-        for (int t = 0; t < kTok; ++t)
-            if (in && chunk >= first && t0 + t < a.T) {
-                if (!SUMMARY) rx[t] = *reinterpret_cast<const raw*>(x + (long long)(t0 + t) * a.xs[1]);
-                rz[t] = *reinterpret_cast<const raw*>(z + (long long)(t0 + t) * a.gs[1]);
-                rd[t] = *reinterpret_cast<const raw*>(dy + (long long)(t0 + t) * a.ys[1]);
-            }
-        if (!SUMMARY && in && chunk >= first)
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) hs[v] = a.saved[((long long)b * chunks + chunk) * a.C + c0 + v];
-    };
-    load(end - 1);
-    float u0[VEC], total[VEC];
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) {
-        u0[v] = !SUMMARY && a.dh_out && in ? a.dh_out[(long long)b * a.C + c0 + v] : 0.0f;
-        total[v] = 1.0f;
-    }
+    st.fetch((end - 1) & 1, rest_rows);
+    N u0 = N::all(0.0f), total = N::all(1.0f), hs = N::all(0.0f);      // hs: h before the chunk
     if (!SUMMARY && in) {
+        hs = load_state<VEC>(saved);
+        if (a.dh_out) u0 = load_state<VEC>(a.dh_out + state);
 #pragma unroll 4
-        for (int s = a.segs - 1; s > seg; --s) {
-            const float* w = a.ws + ((long long)b * a.segs + s) * 2 * a.C + c0;
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) u0[v] = fmaf(w[v], u0[v], w[a.C + v]);
+        for (int s = wk.segs - 1; s > wk.seg; --s) {
+            const float* w = wk.span(a, s) + lane * VEC;
+            u0 = fma(load_state<VEC>(w), u0, load_state<VEC>(w + LC * VEC));
         }
     }
     for (int chunk = end - 1; chunk >= first; --chunk) {
-        const int buf = chunk & 1, t0 = chunk * kScanChunk + slot * kTok;
-        float la[kTok][VEC], A[VEC], H[VEC], Q[VEC], h[VEC];
-        float xv[SUMMARY ? 1 : kTok][VEC], rest[SUMMARY ? 1 : kTok][VEC], dv[kTok][VEC];
-        unsigned ends = 0;
-        RowWalk row(a.t0 + t0, a.grid_w, a.prefix_len);
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) A[v] = 1.0f, H[v] = 0.0f, Q[v] = 0.0f, h[v] = hs[v];
+        const int buf = chunk & 1;
+        N h = hs;
+        if (chunk > first) {
+            __syncwarp();                          // (dy of the chunk before this one has been read)
+            st.move(-1);
+            st.fetch(buf ^ 1, rest_rows + kScanChunk);
+            saved -= a.C;
+            if (!SUMMARY && in) hs = load_state<VEC>(saved);
+        }
+        st.landed(chunk == first);
+        N ca[kTok], rest[kTok], xv[SUMMARY ? 1 : kTok];
 #pragma unroll
         for (int t = 0; t < kTok; ++t) {
-            const bool e = row.step(), live = in && t0 + t < a.T;
-            if (e) ends |= 1u << t;
-            float zv[VEC];
-            P::get(rz[t], zv);
-            P::get(rd[t], dv[t]);
-            if (!SUMMARY) P::get(rx[t], xv[t]);
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) {
-                float lam, r;
-                gate_of(zv[v], LOGITS, lam, r);
-                la[t][v] = live ? lam : 1.0f;
-                if (!live) dv[t][v] = 0.0f;
-                const float ca = e ? 1.0f : la[t][v];
-                A[v] *= ca;
-                if (!SUMMARY) {
-                    rest[t][v] = r;
-                    if (!live) xv[t][v] = 0.0f, rest[t][v] = 0.0f;
-                    H[v] = fmaf(ca, H[v], a.tied ? rest[t][v] * xv[t][v] : xv[t][v]);
-                }
-            }
+            gate_of<LOGITS>(P::get(st.get(buf, 0, t)), ca[t], rest[t]);
+            if constexpr (!SUMMARY) xv[t] = P::get(st.get(buf, 2, t));
         }
-#pragma unroll
-        for (int t = kTok - 1; t >= 0; --t)
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) Q[v] = ((ends >> t) & 1u ? 1.0f : la[t][v]) * (Q[v] + dv[t][v]);
-        load(chunk - 1);
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-            pair[buf][slot][lane * VEC + v] = make_float2(A[v], Q[v]);
-            if (!SUMMARY) fwd[buf][slot][lane * VEC + v] = H[v];
-        }
-        __syncthreads();
-        float u[VEC];
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) u[v] = chunk == end - 1 ? u0[v] : next[buf][lane * VEC + v];
-        for (int s = kSlots - 1; s > slot; --s)
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) {
-                const float2 m = pair[buf][s][lane * VEC + v];
-                u[v] = fmaf(m.x, u[v], m.y);
-                if (SUMMARY && slot == 0) total[v] *= m.x;
-            }
-        if (!SUMMARY)
-            for (int s = 0; s < slot; ++s)
-#pragma unroll
-                for (int v = 0; v < VEC; ++v)
-                    h[v] = fmaf(pair[buf][s][lane * VEC + v].x, h[v], fwd[buf][s][lane * VEC + v]);
-        if (slot == 0)
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) {
-                const float before = fmaf(A[v], u[v], Q[v]);
-                if (SUMMARY) total[v] *= A[v];
-                next[buf ^ 1][lane * VEC + v] = before;
-                if (chunk == first && in) {
-                    if (SUMMARY) {
-                        float* w = a.ws + ((long long)b * a.segs + seg) * 2 * a.C + c0 + v;
-                        w[0] = total[v];
-                        w[a.C] = before;
-                    } else if (first == 0 && a.dh_in) {
-                        a.dh_in[(long long)b * a.C + c0 + v] = before;
-                    }
-                }
-            }
-        if (!SUMMARY && in) {
-            float prev[kTok][VEC];
+        const unsigned ends = rows.mask();
+        if (ends)
 #pragma unroll
             for (int t = 0; t < kTok; ++t)
+                if ((ends >> t) & 1u) ca[t] = N::all(1.0f);
+        if (left < kTok)                           // a token past the end changes nothing (its dy is 0 below)
 #pragma unroll
-                for (int v = 0; v < VEC; ++v) {
-                    prev[t][v] = h[v];
-                    h[v] = fmaf((ends >> t) & 1u ? 1.0f : la[t][v], h[v], a.tied ? rest[t][v] * xv[t][v] : xv[t][v]);
+            for (int t = 0; t < kTok; ++t)
+                if (t >= left) {
+                    ca[t] = N::all(1.0f), rest[t] = N::all(0.0f);
+                    if constexpr (!SUMMARY) xv[t] = N::all(0.0f);
                 }
+        auto grad = [&](int t) { return t < left ? P::get(st.get(buf, 1, t)) : N::all(0.0f); };
+        N A = ca[0], H = N::all(0.0f), Q = N::all(0.0f);
 #pragma unroll
-            for (int t = kTok - 1; t >= 0; --t) {
-                float ox[VEC], og[VEC];
+        for (int t = 1; t < kTok; ++t) A = A * ca[t];
+        if constexpr (!SUMMARY)
 #pragma unroll
-                for (int v = 0; v < VEC; ++v) {
-                    const float g = u[v] + dv[t][v];
-                    const bool e = (ends >> t) & 1u;
-                    u[v] = (e ? 1.0f : la[t][v]) * g;
-                    ox[v] = a.tied ? rest[t][v] * g : g;
-                    float d = (e ? 0.0f : prev[t][v]) - (a.tied ? xv[t][v] : 0.0f);
-                    if (LOGITS) d *= rest[t][v] * la[t][v];      // the derivative of the sigmoid
-                    og[v] = d * g;
-                }
-                if (t0 + t < a.T) {
-                    *reinterpret_cast<raw*>(dx + (long long)(t0 + t) * a.dxs[1]) = P::put(ox);
-                    *reinterpret_cast<raw*>(dg + (long long)(t0 + t) * a.dgs[1]) = P::put(og);
+            for (int t = 0; t < kTok; ++t) H = fma(ca[t], H, TIED ? rest[t] * xv[t] : xv[t]);
+#pragma unroll
+        for (int t = kTok - 1; t >= 0; --t) Q = ca[t] * (Q + grad(t));
+        back[buf][slot][lane] = {A, Q};
+        if (!SUMMARY) fwd[buf][slot][lane] = H;
+        __syncthreads();
+        N u = chunk == end - 1 ? u0 : next[buf][lane];
+#pragma unroll 5
+        for (int s = kSlots - 1; s > slot; --s) {
+            const Span m = back[buf][s][lane];
+            u = fma(m.A, u, m.X);
+            if (SUMMARY && slot == 0) total = total * m.A;
+        }
+        if (!SUMMARY)
+#pragma unroll 5
+            for (int s = 0; s < slot; ++s) h = fma(back[buf][s][lane].A, h, fwd[buf][s][lane]);
+        if (slot == 0) {
+            const N before = fma(A, u, Q);
+            if (SUMMARY) total = total * A;
+            next[buf ^ 1][lane] = before;
+            if (chunk == first && in) {
+                if (SUMMARY) {
+                    float* w = wk.span(a, wk.seg) + lane * VEC;
+                    store_state<VEC>(w, total);
+                    store_state<VEC>(w + LC * VEC, before);
+                } else if (first == 0 && a.dh_in) {
+                    store_state<VEC>(a.dh_in + state, before);
                 }
             }
         }
+        if constexpr (!SUMMARY) {
+            // dlambda_t = g_t f_t, f_t = h_{t-1} - x_t (tied): f_t takes x_t's place
+            const N minus = N::all(-1.0f);
+#pragma unroll
+            for (int t = 0; t < kTok; ++t) {
+                const N prev = h;
+                h = fma(ca[t], h, TIED ? rest[t] * xv[t] : xv[t]);
+                N f = TIED ? fma(xv[t], minus, prev) : prev;
+                if (LOGITS) f = f * (rest[t] * ca[t]);             // the derivative of the sigmoid
+                if (ends && ((ends >> t) & 1u)) {
+                    // a row's last token does not pass h on through lambda; ca is 1 there, and lambda
+                    // is formed again (2^-24 off at most, as the term it scales is)
+                    f = TIED ? xv[t] * minus : N::all(0.0f);
+                    if (LOGITS) f = f * (rest[t] * fma(rest[t], minus, N::all(1.0f)));
+                }
+                xv[t] = f;
+            }
+            if (in)
+#pragma unroll
+                for (int t = kTok - 1; t >= 0; --t) {
+                    const N g = u + grad(t);
+                    u = ca[t] * g;
+                    if (t < left) {
+                        *reinterpret_cast<raw*>(dx + t * a.dxs[1]) = P::put(TIED ? rest[t] * g : g);
+                        *reinterpret_cast<raw*>(dg + t * a.dgs[1]) = P::put(xv[t] * g);
+                    }
+                }
+            dx -= kScanChunk * a.dxs[1];
+            dg -= kScanChunk * a.dgs[1];
+        }
+        rest_rows += kScanChunk;
+        left += kScanChunk;
+        rows.back();
     }
 }
 
@@ -350,16 +569,14 @@ __global__ void __launch_bounds__(256) scan_step_kernel(const ScanArgs a)
     const long long i = a.pos ? (long long)a.pos[b] : a.t0;
     RowWalk row(i, a.grid_w, a.prefix_len);
     const bool ends = row.step();
-    float x[VEC], z[VEC], h[VEC];
-    P::get(*reinterpret_cast<const raw*>(static_cast<const T*>(a.x) + b * a.xs[0] + c), x);
-    P::get(*reinterpret_cast<const raw*>(static_cast<const T*>(a.gate) + b * a.gs[0] + c), z);
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) {
-        float lam, rest;
-        gate_of(z[v], a.logits, lam, rest);
-        h[v] = fmaf(ends ? 1.0f : lam, a.h_in[(long long)b * a.C + c + v], a.tied ? rest * x[v] : x[v]);
-        a.h_out[(long long)b * a.C + c + v] = h[v];
-    }
+    typedef num<VEC> N;
+    const N x = P::get(*reinterpret_cast<const raw*>(static_cast<const T*>(a.x) + b * a.xs[0] + c));
+    const N z = P::get(*reinterpret_cast<const raw*>(static_cast<const T*>(a.gate) + b * a.gs[0] + c));
+    N lam, rest;
+    if (a.logits) gate_of<true>(z, lam, rest);
+    else gate_of<false>(z, lam, rest);
+    const N h = fma(ends ? N::all(1.0f) : lam, load_state<VEC>(a.h_in + (long long)b * a.C + c), a.tied ? rest * x : x);
+    store_state<VEC>(a.h_out + (long long)b * a.C + c, h);
     *reinterpret_cast<raw*>(static_cast<T*>(a.y) + b * a.ys[0] + c) = P::put(h);
 }
 
@@ -376,58 +593,95 @@ bool pairs_ok(const ScanArgs& a)
     return (a.C & 1) == 0;
 }
 
-template <typename T, int VEC, int LC>
-cudaError_t forward_t(const ScanArgs& a, cudaStream_t st)
+// Whether every tensor that is read has rows of whole 16-byte pieces.
+bool wide_ok(const ScanArgs& a)
 {
-    const unsigned tiles = (unsigned)((a.C + LC * VEC - 1) / (LC * VEC)) * a.B;
-    cudaError_t e = cudaSuccess;
-    if (a.segs > 1)
-        e = launch_dependent(a.logits ? scan_forward_kernel<T, VEC, LC, true, true> : scan_forward_kernel<T, VEC, LC, false, true>,
-                             dim3(tiles, a.segs - 1), dim3(LC * kSlots), 0, st, a);
-    if (e != cudaSuccess) return e;
-    return launch_dependent(a.logits ? scan_forward_kernel<T, VEC, LC, true, false> : scan_forward_kernel<T, VEC, LC, false, false>,
-                            dim3(tiles, a.segs), dim3(LC * kSlots), 0, st, a);
+    const long long per = a.bf16 ? 8 : 4;
+    const void* ptrs[] = {a.x, a.gate, a.dy};
+    for (const void* p : ptrs)
+        if (reinterpret_cast<uintptr_t>(p) % 16) return false;
+    const long long* strides[] = {a.xs, a.gs, a.ys};
+    for (int i = 0; i < (a.dy ? 3 : 2); ++i)
+        if (strides[i][0] % per || strides[i][1] % per) return false;
+    return a.C % per == 0;
 }
-template <typename T, int VEC, int LC>
-cudaError_t backward_t(const ScanArgs& a, cudaStream_t st)
+
+template <typename T, int VEC, int LC, bool WIDE, bool LOGITS, bool TIED, bool SUMMARY>
+cudaError_t launch_one(const ScanArgs& a, dim3 grid, cudaStream_t st)
 {
-    const unsigned tiles = (unsigned)((a.C + LC * VEC - 1) / (LC * VEC)) * a.B;
-    cudaError_t e = cudaSuccess;
-    if (a.segs > 1)
-        e = launch_dependent(a.logits ? scan_backward_kernel<T, VEC, LC, true, true> : scan_backward_kernel<T, VEC, LC, false, true>,
-                             dim3(tiles, a.segs - 1), dim3(LC * kSlots), 0, st, a);
-    if (e != cudaSuccess) return e;
-    return launch_dependent(a.logits ? scan_backward_kernel<T, VEC, LC, true, false> : scan_backward_kernel<T, VEC, LC, false, false>,
-                            dim3(tiles, a.segs), dim3(LC * kSlots), 0, st, a);
+    static bool done[2][64];
+    const size_t bytes = Stage<T, VEC, LC, 2, WIDE>::kBytes, bytes3 = Stage<T, VEC, LC, SUMMARY ? 2 : 3, WIDE>::kBytes;
+    if (a.dy) {
+        const cudaError_t e = tcx::allow_dynamic_smem(scan_backward_kernel<T, VEC, LC, WIDE, LOGITS, TIED, SUMMARY>, bytes3, done[1]);
+        return e != cudaSuccess ? e : launch_dependent(scan_backward_kernel<T, VEC, LC, WIDE, LOGITS, TIED, SUMMARY>, grid,
+                                                       dim3(LC * kSlots), bytes3, st, a);
+    }
+    const cudaError_t e = tcx::allow_dynamic_smem(scan_forward_kernel<T, VEC, LC, WIDE, LOGITS, TIED, SUMMARY>, bytes, done[0]);
+    return e != cudaSuccess ? e : launch_dependent(scan_forward_kernel<T, VEC, LC, WIDE, LOGITS, TIED, SUMMARY>, grid,
+                                                   dim3(LC * kSlots), bytes, st, a);
+}
+template <typename T, int VEC, int LC, bool WIDE, bool LOGITS, bool TIED>
+cudaError_t launch_t(const ScanArgs& a, cudaStream_t st)
+{
+    const int tiles = (a.C + LC * VEC - 1) / (LC * VEC) * a.B, cuts = tiles - a.whole;
+    if (a.segs > 1) {
+        const cudaError_t e = launch_one<T, VEC, LC, WIDE, LOGITS, TIED, true>(a, dim3(cuts * (a.segs - 1)), st);
+        if (e != cudaSuccess) return e;
+    }
+    return launch_one<T, VEC, LC, WIDE, LOGITS, TIED, false>(a, dim3(a.whole + cuts * a.segs), st);
+}
+template <typename T, int VEC, int LC, bool WIDE>
+cudaError_t launch_v(const ScanArgs& a, cudaStream_t st)
+{
+    if (a.logits) return a.tied ? launch_t<T, VEC, LC, WIDE, true, true>(a, st) : launch_t<T, VEC, LC, WIDE, true, false>(a, st);
+    return a.tied ? launch_t<T, VEC, LC, WIDE, false, true>(a, st) : launch_t<T, VEC, LC, WIDE, false, false>(a, st);
+}
+// Pairs of channels, 16 lanes of them, and 16-byte copies where the memory allows them; single
+// channels, 32 lanes, elsewhere.
+cudaError_t launch(const ScanArgs& a, cudaStream_t st)
+{
+    if (pairs_ok(a) && wide_ok(a)) return a.bf16 ? launch_v<__nv_bfloat16, 2, 16, true>(a, st) : launch_v<float, 2, 16, true>(a, st);
+    return a.bf16 ? launch_v<__nv_bfloat16, 1, 32, false>(a, st) : launch_v<float, 1, 32, false>(a, st);
 }
 
 }  // namespace
 
-// How a call's work is cut.  Tiles are 16 lanes wide; a sequence is cut into segments until there
-// are about four CTAs per SM.
-void scan_plan(ScanArgs& a, int sms)
+// How a call's work is cut.  A tile is 32 channels of one sequence, `slots` the CTAs that run at a time.
+// Fewer tiles than half the slots: all of them are cut, into as many segments as there are slots
+// for.  A last round of tiles that would leave half of the slots idle or more: the tiles of that round
+// are cut.  A segment's summary reads two of the forward's three and the backward's five streams
+// once more (from L2 where the call fits it), which the fuller rounds pay for.
+// The forward of 1 x 9217 x 1536: 45 us cut into 9, 300 us whole.
+void scan_plan(ScanArgs& a, bool backward, int sms)
 {
-    const int width = 16 * 2;
-    const long long tiles = (long long)a.B * ((a.C + width - 1) / width);
+    const long long tiles = (long long)a.B * ((a.C + 31) / 32);
     const int chunks = (a.T + kScanChunk - 1) / kScanChunk;
-    long long segs = tiles >= sms ? 1 : (4LL * sms + tiles - 1) / tiles;
-    if (segs > chunks) segs = chunks;
-    a.seg_chunks = (int)((chunks + segs - 1) / segs);
-    a.segs = (chunks + a.seg_chunks - 1) / a.seg_chunks;
+    const long long slots = (long long)sms * (a.bf16 ? backward ? 2 : 3 : backward ? 1 : 2);
+    long long whole = tiles, segs = 1;
+    if (tiles * 2 <= slots) {
+        whole = 0;
+    } else if (tiles > slots && tiles < 4 * slots && tiles % slots * 2 <= slots) {
+        whole = tiles - tiles % slots;
+    }
+    if (whole < tiles) {
+        segs = slots / (tiles - whole);
+        if (segs > chunks) segs = chunks;
+        a.seg_chunks = (int)((chunks + segs - 1) / segs);
+        segs = (chunks + a.seg_chunks - 1) / a.seg_chunks;
+    }
+    if (segs == 1) whole = tiles;
+    a.whole = (int)whole;
+    a.segs = (int)segs;
 }
-size_t scan_workspace_bytes(const ScanArgs& a) { return a.segs > 1 ? (size_t)a.B * a.segs * 2 * a.C * sizeof(float) : 0; }
+size_t scan_workspace_bytes(const ScanArgs& a)
+{
+    const size_t tiles = (size_t)a.B * ((a.C + 31) / 32);
+    return a.segs > 1 ? (tiles - a.whole) * a.segs * 2 * 32 * sizeof(float) : 0;
+}
 int scan_launches(const ScanArgs& a) { return a.segs > 1 ? 2 : 1; }
 
-cudaError_t launch_scan_forward(const ScanArgs& a, cudaStream_t st)
-{
-    if (pairs_ok(a)) return a.bf16 ? forward_t<__nv_bfloat16, 2, 16>(a, st) : forward_t<float, 2, 16>(a, st);
-    return a.bf16 ? forward_t<__nv_bfloat16, 1, 32>(a, st) : forward_t<float, 1, 32>(a, st);
-}
-cudaError_t launch_scan_backward(const ScanArgs& a, cudaStream_t st)
-{
-    if (pairs_ok(a)) return a.bf16 ? backward_t<__nv_bfloat16, 2, 16>(a, st) : backward_t<float, 2, 16>(a, st);
-    return a.bf16 ? backward_t<__nv_bfloat16, 1, 32>(a, st) : backward_t<float, 1, 32>(a, st);
-}
+cudaError_t launch_scan_forward(const ScanArgs& a, cudaStream_t st) { return launch(a, st); }     // (a.dy is null)
+cudaError_t launch_scan_backward(const ScanArgs& a, cudaStream_t st) { return launch(a, st); }
 cudaError_t launch_scan_step(const ScanArgs& a, cudaStream_t st)
 {
     const bool pairs = pairs_ok(a);

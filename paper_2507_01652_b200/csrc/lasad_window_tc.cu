@@ -208,7 +208,7 @@ window_forward_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
         const int row = warp * 32 + lane, t = q0 + row;
         const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
         const int tw0 = q0 + warp * 32, tw1 = tw0 + 31;          // the warp's queries
-        float m = -INFINITY, l0 = 0.0f, l1 = 0.0f;
+        float m = -INFINITY, l[4] = {0.0f, 0.0f, 0.0f, 0.0f};     // (four sums: no long chain of additions)
         bool ok = true;
         for (int j = 0; j < n; ++j) {
             const int k0 = tile_of(j) * kRows, blocks = blocks_of(j);
@@ -230,7 +230,7 @@ window_forward_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
             tmem_wait_ld();
             tc_fence_before();
             mbar_arrive(&sm.s_free);
-            float top = -INFINITY;
+            float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 if (vis[c] == 1) {
@@ -241,9 +241,10 @@ window_forward_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
                 }
                 if (vis[c])
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) top = fmaxf(top, __uint_as_float(sv[c][e]));
+                    for (int e = 0; e < 32; e += 2)
+                        tops[(e >> 1) & 3] = max3(tops[(e >> 1) & 3], __uint_as_float(sv[c][e]), __uint_as_float(sv[c][e + 1]));
             }
-            top *= p.scale2;
+            const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * p.scale2;
             // P of the tile before has been used, and O is complete up to it
             if (j > 0 && !(ok = warp_wait(&sm.o_done, (j - 1) & 1, limit, abort_flag, p.status))) break;
             tc_fence_after();
@@ -253,8 +254,8 @@ window_forward_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
             } else if (__any_sync(0xffffffffu, grow)) {
                 const float now = grow ? top : m, f = grow ? ex2_approx(m - now) : 1.0f;
                 m = now;
-                l0 *= f;
-                l1 *= f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) l[e] *= f;
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     uint32_t o[16];
@@ -277,8 +278,7 @@ window_forward_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
                         fma2s(__uint_as_float(sv[c][2 * e]), __uint_as_float(sv[c][2 * e + 1]), p.scale2, base, x0, x1);
                         x0 = ex2_approx(x0);
                         x1 = ex2_approx(x1);
-                        l0 += x0;
-                        l1 += x1;
+                        add2(l[(e & 1) * 2], l[(e & 1) * 2 + 1], x0, x1);
                         pk[e] = pack_bf16(x0, x1);
                     }
                 } else {
@@ -300,11 +300,11 @@ window_forward_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
         if (ok && n > 0) ok = warp_wait(&sm.o_done, (n - 1) & 1, limit, abort_flag, p.status);
         if (ok) {
             tc_fence_after();
-            const float l = l0 + l1;
-            const bool none = t >= len || l == 0.0f;
-            const float inv = none ? 0.0f : 1.0f / l;
+            const float sum = (l[0] + l[1]) + (l[2] + l[3]);
+            const bool none = t >= len || sum == 0.0f;
+            const float inv = none ? 0.0f : 1.0f / sum;
             if (p.lse && t < p.T)
-                p.lse[(long long)bh * p.T + t] = none ? -INFINITY : m * kLn2 + logf(l);
+                p.lse[(long long)bh * p.T + t] = none ? -INFINITY : m * kLn2 + logf(sum);
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 uint32_t o[32];

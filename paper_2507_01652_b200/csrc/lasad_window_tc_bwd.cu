@@ -17,13 +17,15 @@
 // over the queries whose window has left them come from launch_window_prep.
 //
 // What bounds it: per tile 512 clocks of exponentials (16 per SM and clock) against four (three)
-// products of 128 clocks.  Two groups of four warps take the tiles in turn, each with its own S
+// products of 128 clocks.  Two groups of eight warps take the tiles in turn, each with its own S
 // and dP columns, so that one group's exponentials run under the other's products: 448 (384) of
 // the SM's 512 TMEM columns, one CTA per SM.  Against one kernel that makes all five products once
 // and adds dQ by atomics this makes S, dP and P twice; it buys results that repeat, and no 32-bit dQ in
 // memory.
 //
-// Warps 0-3 and 4-7: the two groups, one thread per own row.  Warp 8: MMA issue.  Warp 9: TMA.
+// Warps 0-7 and 8-15: the two groups, two threads per own row, 32 of a tile's 64 columns each (a
+// group of four warps with 64 columns each left a scheduler two warps, too few to hide the
+// latency of TMEM and of the exponentials).  Warp 16: MMA issue.  Warp 17: TMA.
 #include "lasad_window_tma.cuh"
 
 namespace lasad {
@@ -31,7 +33,7 @@ namespace {
 
 using namespace tcx;
 
-constexpr int kRows = 128, kCols = 64, kStages = 4, kThreads = 320;
+constexpr int kRows = 128, kCols = 64, kStages = 4, kGroup = 256, kThreads = 2 * kGroup + 64;
 constexpr int kTile = kCols * 128;                         // bytes of a passing tile
 constexpr uint32_t kColX1 = 0, kColX2 = 32, kColS = 64, kColDP = 128, kGroupCols = 128, kColA1 = 320, kColA2 = 384;
 constexpr int kTmemCols = 512;
@@ -41,10 +43,10 @@ struct Smem {
     unsigned char y2[kStages][kTile];
     float lse[2][2][kCols], delta[2][2][kCols];            // keys: of each group's tiles, by column, two in turn
     unsigned long long full[kStages], free[kStages];       // Y1 and Y2 have landed; their products have been made
-    unsigned long long x_ready;                            // X1 and X2 are in TMEM (256 arrivals)
+    unsigned long long x_ready;                            // X1 and X2 are in TMEM (2 kGroup arrivals)
     unsigned long long s_full[2];                          // S and dP of a group's tile are there
-    unsigned long long p_ready[2];                         // P and dS are (128 arrivals)
-    unsigned long long st_ready[2];                        // keys: lse and delta are (128 arrivals)
+    unsigned long long p_ready[2];                         // P and dS are (kGroup arrivals)
+    unsigned long long st_ready[2];                        // keys: lse and delta are (kGroup arrivals)
     unsigned long long done, drain;
     uint32_t tmem_base;
     int abort_flag;
@@ -67,20 +69,17 @@ struct Params {
     unsigned wait_limit;
 };
 
-// One 64-channel row of an own operand into 32 TMEM columns.
-__device__ __forceinline__ void row_to_tmem(uint32_t col, const __nv_bfloat16* row, bool live, int d)
+// 32 channels of a row of an own operand into 16 TMEM columns.
+__device__ __forceinline__ void half_row_to_tmem(uint32_t col, const __nv_bfloat16* row, bool live)
 {
+    uint32_t r[16];
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-        uint32_t r[16];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (live && 32 * c + 8 * i < d) v = *reinterpret_cast<const uint4*>(row + 32 * c + 8 * i);
-            r[4 * i] = v.x, r[4 * i + 1] = v.y, r[4 * i + 2] = v.z, r[4 * i + 3] = v.w;
-        }
-        tmem_st16(col + 16 * c, r);
+    for (int i = 0; i < 4; ++i) {
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (live) v = *reinterpret_cast<const uint4*>(row + 8 * i);
+        r[4 * i] = v.x, r[4 * i + 1] = v.y, r[4 * i + 2] = v.z, r[4 * i + 3] = v.w;
     }
+    tmem_st16(col, r);
 }
 
 template <bool KEYS>
@@ -103,11 +102,11 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
             mbar_init(&sm.full[s], 1);
             mbar_init(&sm.free[s], 1);
         }
-        mbar_init(&sm.x_ready, 256);
+        mbar_init(&sm.x_ready, 2 * kGroup);
         for (int w = 0; w < 2; ++w) {
             mbar_init(&sm.s_full[w], 1);
-            mbar_init(&sm.p_ready[w], 128);
-            mbar_init(&sm.st_ready[w], 128);
+            mbar_init(&sm.p_ready[w], kGroup);
+            mbar_init(&sm.st_ready[w], kGroup);
         }
         mbar_init(&sm.done, 1);
         mbar_init(&sm.drain, 1);
@@ -116,7 +115,7 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
     }
     // (TMEM only after the kernel before has ended, the next kernel only after the TMEM: see the forward)
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (warp == 8) {
+    if (warp == 16) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm.tmem_base)),
                      "r"(kTmemCols)
                      : "memory");
@@ -147,7 +146,7 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
     auto first_of = [&](int i) { return (KEYS ? lo + i % per : i < extra ? i : lo + i - extra) * kCols; };
     auto head_of = [&](int i) { return KEYS ? h * G + i / per : h / G; };
 
-    if (warp == 9) {
+    if (warp == 17) {
         if (elect_one()) {
             int issued = 0;
             for (; issued < n; ++issued) {
@@ -163,7 +162,7 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
                     if (mbar_try_wait(&sm.full[j % kStages], (j / kStages) & 1)) break;
         }
         __syncwarp();
-    } else if (warp == 8) {
+    } else if (warp == 16) {
         const uint64_t dy1 = make_desc(smem_u32(sm.y1[0])), dy2 = make_desc(smem_u32(sm.y2[0]));
         constexpr uint64_t stage = kTile >> 4;
         constexpr uint32_t idesc_s = make_idesc(128, 64, 0, 0);    // X (tmem) x Y (K-major)
@@ -193,10 +192,11 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
                 if (KEYS)
 #pragma unroll
                     for (int kk = 0; kk < 4; ++kk)       // 16 passing rows: 8 columns of P, 2048 bytes of Y
-                        mma_ts(tmem + kColA2, at_p + 8 * kk, dy2 + s * stage + 128 * kk, idesc_a, i > 0 || kk > 0);
+                                                         // (rows 32-63 stand 32 columns on)
+                        mma_ts(tmem + kColA2, at_p + 32 * (kk >> 1) + 8 * (kk & 1), dy2 + s * stage + 128 * kk, idesc_a, i > 0 || kk > 0);
 #pragma unroll
                 for (int kk = 0; kk < 4; ++kk)
-                    mma_ts(tmem + kColA1, at_ds + 8 * kk, dy1 + s * stage + 128 * kk, idesc_a, i > 0 || kk > 0);
+                    mma_ts(tmem + kColA1, at_ds + 32 * (kk >> 1) + 8 * (kk & 1), dy1 + s * stage + 128 * kk, idesc_a, i > 0 || kk > 0);
                 mma_commit(&sm.free[s]);
                 if (i == n - 1) mma_commit(&sm.done);
             }
@@ -211,14 +211,16 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
         }
         __syncwarp();
     } else {
-        const int group = warp >> 2, row = (warp & 3) * 32 + lane, r = r0 + row, gt = tid & 127;
+        const int group = warp >> 3, c = (warp >> 2) & 1;         // c: which 32 of the columns
+        const int row = (warp & 3) * 32 + lane, r = r0 + row, gt = tid & (kGroup - 1);
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const int rw0 = r0 + (warp & 3) * 32, rw1 = rw0 + 31;     // the warp's rows
-        const int own_head = h;
-        if (group == 0)
-            row_to_tmem(lanes + kColX1, p.x1 + b * p.x1s[0] + r * p.x1s[1] + own_head * p.x1s[2], r < len, p.d);
-        else
-            row_to_tmem(lanes + kColX2, p.x2 + b * p.x2s[0] + r * p.x2s[1] + own_head * p.x2s[2], r < len, p.d);
+        // X1 by group 0, X2 by group 1, half a row each
+        {
+            const __nv_bfloat16* x = group == 0 ? p.x1 + b * p.x1s[0] + r * p.x1s[1] + h * p.x1s[2]
+                                                : p.x2 + b * p.x2s[0] + r * p.x2s[1] + h * p.x2s[2];
+            half_row_to_tmem(lanes + (group == 0 ? kColX1 : kColX2) + 16 * c, x + 32 * c, r < len && 32 * c < p.d);
+        }
         tmem_wait_st();
         tc_fence_before();
         mbar_arrive(&sm.x_ready);
@@ -228,10 +230,10 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
             row_lse = -p.lse[(long long)bh * p.T + r] * kLog2e;
             row_delta = -p.delta[(long long)bh * p.T + r];
         }
-        // keys: this thread's part of the tile's 64 lse (threads 0-63) and Delta (64-127), one tile ahead
+        // keys: this thread's part of the tile's 64 lse (threads 0-63) and Delta (64-127; the rest has none), one tile ahead
         auto stat = [&](int i) {
             const int q = first_of(i) + (gt & 63);
-            if (q >= len) return 0.0f;
+            if (gt >= 128 || q >= len) return 0.0f;
             const long long x = ((long long)b * p.Hq + head_of(i)) * p.T + q;
             return gt < 64 ? -p.lse[x] * kLog2e : -p.delta[x];
         };
@@ -241,7 +243,7 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
             const int s = i % kStages, c0 = first_of(i);
             if (KEYS) {
                 // (a buffer is written again two tiles on, when every thread has arrived for the one between)
-                (gt < 64 ? sm.lse : sm.delta)[group][(i >> 1) & 1][gt & 63] = ahead;
+                if (gt < 128) (gt < 64 ? sm.lse : sm.delta)[group][(i >> 1) & 1][gt & 63] = ahead;
                 mbar_arrive(&sm.st_ready[group]);
                 if (i + 2 < n) ahead = stat(i + 2);
                 if (!(ok = warp_wait(&sm.st_ready[group], (i >> 1) & 1, limit, abort_flag, p.status))) break;
@@ -249,8 +251,7 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
             if (!(ok = warp_wait(&sm.s_full[group], (i >> 1) & 1, limit, abort_flag, p.status))) break;
             tc_fence_after();
             const uint32_t at_s = lanes + kColS + group * kGroupCols, at_dp = lanes + kColDP + group * kGroupCols;
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
+            {
                 // what the warp's rows and these 32 columns have to do with each other: 0 nothing, 1 part, 2 all
                 const int s0 = c0 + 32 * c, s1 = s0 + 31;
                 bool any, all;
@@ -267,13 +268,9 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
                     tmem_ld32(at_s + 32 * c, sv);
                     tmem_ld32(at_dp + 32 * c, dv);
                     tmem_wait_ld();
-                    uint32_t bits = 0xffffffffu;
-                    if (!all)
-                        bits = r >= len ? 0u : KEYS ? bit_range(r - s0, min(r + p.window - 1, len - 1) - s0)
-                                                    : seen_bits(r, s0, p.window, p.sinks, len);
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        float x0, x1, g0, g1, m0, m1;
+                        float x0, x1, g0 = __uint_as_float(dv[2 * e]), g1 = __uint_as_float(dv[2 * e + 1]);
                         float2 ls = make_float2(row_lse, row_lse), de = make_float2(row_delta, row_delta);
                         if (KEYS) {
                             ls = *reinterpret_cast<const float2*>(&sm.lse[group][(i >> 1) & 1][32 * c + 2 * e]);
@@ -282,31 +279,35 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
                         fma2(__uint_as_float(sv[2 * e]), __uint_as_float(sv[2 * e + 1]), p.scale2, ls.x, ls.y, x0, x1);
                         x0 = ex2_approx(x0);
                         x1 = ex2_approx(x1);
-                        g0 = __uint_as_float(dv[2 * e]) + de.x;
-                        g1 = __uint_as_float(dv[2 * e + 1]) + de.y;
-                        m0 = x0 * g0;
-                        m1 = x1 * g1;
-                        if (!all) {
-                            if (!((bits >> (2 * e)) & 1u)) x0 = 0.0f, m0 = 0.0f;
-                            if (!((bits >> (2 * e + 1)) & 1u)) x1 = 0.0f, m1 = 0.0f;
-                        }
+                        add2(g0, g1, de.x, de.y);
+                        mul2_pair(g0, g1, x0, x1);
                         pp[e] = pack_bf16(x0, x1);
-                        pd[e] = pack_bf16(m0, m1);
+                        pd[e] = pack_bf16(g0, g1);
+                    }
+                    if (!all) {          // (what is masked may be NaN: its bits go)
+                        const uint32_t bits = r >= len ? 0u : KEYS ? bit_range(r - s0, min(r + p.window - 1, len - 1) - s0)
+                                                                   : seen_bits(r, s0, p.window, p.sinks, len);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const uint32_t keep = ((bits >> (2 * e)) & 1u ? 0x0000ffffu : 0u) | ((bits >> (2 * e + 1)) & 1u ? 0xffff0000u : 0u);
+                            pp[e] &= keep;
+                            pd[e] &= keep;
+                        }
                     }
                 } else {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) pp[e] = pd[e] = 0u;
                 }
-                // over the columns that this thread has read (block 1's come after block 0's)
-                if (KEYS) tmem_st16(at_s + 16 * c, pp);
-                tmem_st16(at_dp + 16 * c, pd);
+                // over the columns that this thread has read
+                if (KEYS) tmem_st16(at_s + 32 * c, pp);
+                tmem_st16(at_dp + 32 * c, pd);
             }
             // rows past the sequence's end do not count, whatever they hold
             if (len < p.T && c0 + kCols > len) {
                 const int y = gt & 63;
                 if (c0 + y >= len) {
                     if (gt < 64) zero_row(sm.y1[s] + y * 128);
-                    else if (KEYS) zero_row(sm.y2[s] + y * 128);
+                    else if (KEYS && gt < 128) zero_row(sm.y2[s] + y * 128);
                 }
                 fence_proxy_async();
             }
@@ -319,21 +320,20 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
         // group 0: A1 (dK, dQ), times scale; group 1: A2 (dV)
         if (ok && (KEYS || group == 0)) {
             const float f = group == 0 ? p.scale : 1.0f;
-            __nv_bfloat16* out = group == 0 ? p.a1 + b * p.a1s[0] + r * p.a1s[1] + own_head * p.a1s[2]
-                                            : p.a2 + b * p.a2s[0] + r * p.a2s[1] + own_head * p.a2s[2];
+            __nv_bfloat16* out = group == 0 ? p.a1 + b * p.a1s[0] + r * p.a1s[1] + h * p.a1s[2]
+                                            : p.a2 + b * p.a2s[0] + r * p.a2s[1] + h * p.a2s[2];
             const int chunks = (p.T + kPrepRows - 1) / kPrepRows, sinks = min(p.sinks, p.T);
             const float* sums = p.sums + ((long long)bh * chunks * sinks + r) * 2 * p.d + group * p.d;
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
+            {
                 uint32_t a[32];
                 if (n > 0) {
                     tmem_ld32(lanes + (group == 0 ? kColA1 : kColA2) + 32 * c, a);
                     tmem_wait_ld();
                 }
-                if (r >= p.T || 32 * c >= p.d) continue;
+                const bool live = r < p.T && 32 * c < p.d;
 #pragma unroll
                 for (int e = 0; e < 32; ++e) a[e] = n == 0 || r >= len ? 0u : __float_as_uint(__uint_as_float(a[e]) * f);
-                if (KEYS && r < sinks && p.window < len)
+                if (KEYS && live && r < sinks && p.window < len)
                     for (int k = p.window / kPrepRows; k < (len + kPrepRows - 1) / kPrepRows; ++k)
 #pragma unroll
                         for (int e = 0; e < 32; e += 4) {
@@ -343,6 +343,7 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
                             a[e + 2] = __float_as_uint(__uint_as_float(a[e + 2]) + v.z);
                             a[e + 3] = __float_as_uint(__uint_as_float(a[e + 3]) + v.w);
                         }
+                if (live)
 #pragma unroll
                 for (int e = 0; e < 32; e += 8) {
                     uint4 v;
@@ -358,7 +359,7 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
 
     tc_fence_before();
     __syncthreads();
-    if (warp == 8) {
+    if (warp == 16) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
     }

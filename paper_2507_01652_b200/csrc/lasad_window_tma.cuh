@@ -57,6 +57,22 @@ __device__ __forceinline__ void zero_row(unsigned char* row)
     for (int i = 0; i < 8; ++i) p[i] = make_uint4(0, 0, 0, 0);
 }
 
+// the largest of three
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// {a0 + b0, a1 + b1}, in place
+__device__ __forceinline__ void add2(float& a0, float& a1, float b0, float b1)
+{
+    unsigned long long pa, pb;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(pa) : "f"(a0), "f"(a1));
+    asm("mov.b64 %0, {%1, %2};" : "=l"(pb) : "f"(b0), "f"(b1));
+    asm("add.rn.f32x2 %0, %0, %1;" : "+l"(pa) : "l"(pb));
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(a0), "=f"(a1) : "l"(pa));
+}
 // {a0 * b + c, a1 * b + c}
 __device__ __forceinline__ void fma2s(float a0, float a1, float b, float c, float& r0, float& r1)
 {

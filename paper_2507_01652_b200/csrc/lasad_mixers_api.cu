@@ -104,8 +104,9 @@ int rope_args(lasad_ctx* ctx, const lasad_rope_params* p, bool backward, bool ha
         }
         if (last >= p->table_rows) return LASAD_ERR_INVALID_ARG;
     }
-    if ((p->d != 32 && p->d != 64) || (int64_t)p->B * p->T > 0x7fffffffLL) return LASAD_ERR_UNSUPPORTED;
-    if (p->Hq > 65535 || p->Hk > 65535) return LASAD_ERR_UNSUPPORTED;
+    if ((p->d != 32 && p->d != 64) || (int64_t)p->B * p->T > (1 << 30)) return LASAD_ERR_UNSUPPORTED;
+    // (units of a launch are counted in 32 bits)
+    if (p->B > 65535 || (int64_t)p->B * p->T * ((int64_t)p->Hq + p->Hk) > 0x7fffffffLL) return LASAD_ERR_UNSUPPORTED;
     if (on_device(ctx) != LASAD_OK) return LASAD_ERR_INVALID_ARG;
     a.B = p->B, a.T = p->T, a.Hq = p->Hq, a.Hk = p->Hk, a.d = p->d;
     a.grid_w = p->grid_w, a.prefix_len = p->prefix_len, a.t0 = p->t0;

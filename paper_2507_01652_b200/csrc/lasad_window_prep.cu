@@ -34,7 +34,7 @@ __device__ __forceinline__ void load_piece(const T* p, float (&v)[N])
     }
 }
 
-constexpr int kWarps = 8;
+constexpr int kWarps = 8, kAhead = 3;
 
 template <typename T, int D>
 __global__ void __launch_bounds__(32 * kWarps) window_prep_kernel(const WindowArgs a)
@@ -50,18 +50,26 @@ __global__ void __launch_bounds__(32 * kWarps) window_prep_kernel(const WindowAr
     const T* o = static_cast<const T*>(a.o) + b * a.os[0] + sub * N;
     const T* g = static_cast<const T*>(a.dout) + b * a.dos[0] + sub * N;
     const T* q = static_cast<const T*>(a.q) + b * a.qs[0] + sub * N;
-    for (int r = warp * ROWS + mine; r < (rows * G + kWarps * ROWS - 1) / (kWarps * ROWS) * (kWarps * ROWS); r += kWarps * ROWS) {
-        const bool in = r < rows * G;
-        const int t = t0 + (in ? r / G : 0), h = hk * G + (in ? r % G : 0);
-        float ov[N], gv[N], d = 0.0f;
-        load_piece<T, N>(o + t * a.os[1] + h * a.os[2], ov);
-        load_piece<T, N>(g + t * a.dos[1] + h * a.dos[2], gv);
+    // (kAhead rows of each lane group at a time: their loads are in flight together)
+    for (int r0 = 0; r0 < rows * G; r0 += kWarps * ROWS * kAhead) {
+        float ov[kAhead][N], gv[kAhead][N];
 #pragma unroll
-        for (int e = 0; e < N; ++e) d = fmaf(ov[e], gv[e], d);
+        for (int i = 0; i < kAhead; ++i) {
+            const int r = min(r0 + (i * kWarps + warp) * ROWS + mine, rows * G - 1), t = t0 + r / G, h = hk * G + r % G;
+            load_piece<T, N>(o + t * a.os[1] + h * a.os[2], ov[i]);
+            load_piece<T, N>(g + t * a.dos[1] + h * a.dos[2], gv[i]);
+        }
 #pragma unroll
-        for (int k = LANES / 2; k >= 1; k >>= 1) d += __shfl_xor_sync(0xffffffffu, d, k);
-        // (a row past its sequence's end counts for nothing, whatever stands in o and do there)
-        if (in && sub == 0) a.ws[((long long)b * a.Hq + h) * a.T + t] = t < len ? d : 0.0f;
+        for (int i = 0; i < kAhead; ++i) {
+            const int r = r0 + (i * kWarps + warp) * ROWS + mine, t = t0 + r / G, h = hk * G + r % G;
+            float d = 0.0f;
+#pragma unroll
+            for (int e = 0; e < N; ++e) d = fmaf(ov[i][e], gv[i][e], d);
+#pragma unroll
+            for (int k = LANES / 2; k >= 1; k >>= 1) d += __shfl_xor_sync(0xffffffffu, d, k);
+            // (a row past its sequence's end counts for nothing, whatever stands in o and do)
+            if (r < rows * G && sub == 0) a.ws[((long long)b * a.Hq + h) * a.T + t] = t < len ? d : 0.0f;
+        }
     }
     const int sinks = min(a.sinks, a.T);
     if (sinks == 0 || t0 + rows <= a.window || t0 >= len) return;   // (uniform over the CTA)
@@ -77,25 +85,32 @@ __global__ void __launch_bounds__(32 * kWarps) window_prep_kernel(const WindowAr
         for (int e = 0; e < N; ++e) dk[e] = dv[e] = 0.0f;
         const int lo = max(0, s + a.window - t0), hi = min(rows, len - t0);   // rows lo..hi-1 see s as a sink only
         const int n = max(0, hi - lo) * G;
-        for (int r0 = 0; r0 < n; r0 += kWarps * ROWS) {
-            const int r = r0 + warp * ROWS + mine;
-            const bool in = r < n;
-            const int t = t0 + lo + (in ? r / G : 0), h = hk * G + (in ? r % G : 0);
-            float qv[N], gv[N], x = 0.0f, y = 0.0f;
-            load_piece<T, N>(q + t * a.qs[1] + h * a.qs[2], qv);
-            load_piece<T, N>(g + t * a.dos[1] + h * a.dos[2], gv);
+        for (int r0 = 0; r0 < n; r0 += kWarps * ROWS * kAhead) {
+            float qv[kAhead][N], gv[kAhead][N], ls[kAhead], de[kAhead];
 #pragma unroll
-            for (int e = 0; e < N; ++e) x = fmaf(qv[e], kv[e], x), y = fmaf(gv[e], vv[e], y);
-#pragma unroll
-            for (int k = LANES / 2; k >= 1; k >>= 1) {
-                x += __shfl_xor_sync(0xffffffffu, x, k);
-                y += __shfl_xor_sync(0xffffffffu, y, k);
-            }
-            if (in) {
+            for (int i = 0; i < kAhead; ++i) {
+                const int r = min(r0 + (i * kWarps + warp) * ROWS + mine, n - 1), t = t0 + lo + r / G, h = hk * G + r % G;
                 const long long at = ((long long)b * a.Hq + h) * a.T + t;
-                const float p = exp2f((x * a.scale - a.lse[at]) * kLog2e), ds = p * (y - delta[at]) * a.scale;
+                load_piece<T, N>(q + t * a.qs[1] + h * a.qs[2], qv[i]);
+                load_piece<T, N>(g + t * a.dos[1] + h * a.dos[2], gv[i]);
+                ls[i] = a.lse[at];
+                de[i] = delta[at];
+            }
 #pragma unroll
-                for (int e = 0; e < N; ++e) dk[e] = fmaf(ds, qv[e], dk[e]), dv[e] = fmaf(p, gv[e], dv[e]);
+            for (int i = 0; i < kAhead; ++i) {
+                float x = 0.0f, y = 0.0f;
+#pragma unroll
+                for (int e = 0; e < N; ++e) x = fmaf(qv[i][e], kv[e], x), y = fmaf(gv[i][e], vv[e], y);
+#pragma unroll
+                for (int k = LANES / 2; k >= 1; k >>= 1) {
+                    x += __shfl_xor_sync(0xffffffffu, x, k);
+                    y += __shfl_xor_sync(0xffffffffu, y, k);
+                }
+                if (r0 + (i * kWarps + warp) * ROWS + mine < n) {
+                    const float p = exp2f((x * a.scale - ls[i]) * kLog2e), ds = p * (y - de[i]) * a.scale;
+#pragma unroll
+                    for (int e = 0; e < N; ++e) dk[e] = fmaf(ds, qv[i][e], dk[e]), dv[e] = fmaf(p, gv[i][e], dv[e]);
+                }
             }
         }
 #pragma unroll

@@ -647,8 +647,8 @@ cudaError_t launch(const ScanArgs& a, cudaStream_t st)
 }  // namespace
 
 // How a call's work is cut.  A tile is 32 channels of one sequence, `slots` the CTAs that run at a time.
-// Fewer tiles than half the slots: all of them are cut, into as many segments as there are slots
-// for.  A last round of tiles that would leave half of the slots idle or more: the tiles of that round
+// Fewer tiles than half the slots and eight chunks or more (below, the second launch costs what it saves):
+// all of them are cut, into as many segments as there are slots for.  A last round of tiles that would leave half of the slots idle or more: the tiles of that round
 // are cut.  A segment's summary reads two of the forward's three and the backward's five streams
 // once more (from L2 where the call fits it), which the fuller rounds pay for.
 // The forward of 1 x 9217 x 1536: 45 us cut into 9, 300 us whole.
@@ -658,7 +658,8 @@ void scan_plan(ScanArgs& a, bool backward, int sms)
     const int chunks = (a.T + kScanChunk - 1) / kScanChunk;
     const long long slots = (long long)sms * (a.bf16 ? backward ? 2 : 3 : backward ? 1 : 2);
     long long whole = tiles, segs = 1;
-    if (tiles * 2 <= slots) {
+    if (chunks < 8) {
+    } else if (tiles * 2 <= slots) {
         whole = 0;
     } else if (tiles > slots && tiles < 4 * slots && tiles % slots * 2 <= slots) {
         whole = tiles - tiles % slots;

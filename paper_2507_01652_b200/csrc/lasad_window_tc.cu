@@ -65,7 +65,7 @@ window_forward_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
 {
     extern __shared__ unsigned char smem_raw[];
     Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
     volatile int* abort_flag = &sm.abort_flag;
     const unsigned limit = p.wait_limit;
     // the last query tiles, which have the most key tiles, first
@@ -105,9 +105,9 @@ window_forward_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
     __syncthreads();
     tc_fence_after();
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const uint32_t tmem = sm.tmem_base;
+    const uint32_t tmem = (uint32_t)uniform((int)sm.tmem_base);
 
-    const int len = p.lengths ? max(0, min(p.lengths[b], p.T)) : p.T;
+    const int len = uniform(p.lengths ? max(0, min(p.lengths[b], p.T)) : p.T);
     // key tiles of this CTA: the sinks' that lie before the window's, then lo .. hi - 1
     const int hi = q0 >= len ? 0 : (min(q0 + kRows, len) + kCols - 1) / kCols;
     const int lo = min(hi, q0 >= p.window ? (q0 - p.window + 1) / kCols : 0);

@@ -88,7 +88,7 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
 {
     extern __shared__ unsigned char smem_raw[];
     Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
     volatile int* abort_flag = &sm.abort_flag;
     const unsigned limit = p.wait_limit;
     // the CTAs with most tiles first: the first key tiles, the last query tiles
@@ -125,9 +125,9 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
     __syncthreads();
     tc_fence_after();
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const uint32_t tmem = sm.tmem_base;
+    const uint32_t tmem = (uint32_t)uniform((int)sm.tmem_base);
 
-    const int len = p.lengths ? max(0, min(p.lengths[b], p.T)) : p.T;
+    const int len = uniform(p.lengths ? max(0, min(p.lengths[b], p.T)) : p.T);
     // the tiles that pass.  keys: the query tiles r0/64 .. of every head of the group; queries: the
     // sinks' tiles that lie before the window, then the window's
     int per = 0, lo = 0, extra = 0, n = 0;

@@ -43,6 +43,10 @@ __device__ __forceinline__ uint32_t seen_bits(int t, int s0, int window, int sin
     return bit_range(t - window + 1 - s0, last) | bit_range(0, min(last, sinks - 1 - s0));
 }
 
+// A value that all lanes of the warp have, in a form that the compiler knows to be one: addresses and
+// descriptors of tcgen05 instructions built from such values stay in uniform registers.
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
+
 // mbar_wait of a whole warp: every lane goes on, or none does, so that what follows may need all of them.
 __device__ __forceinline__ bool warp_wait(void* bar, unsigned parity, unsigned limit, volatile int* abort_flag, int* status)
 {

@@ -38,7 +38,7 @@ struct Smem {
     unsigned char k[kStages][kTile];           // (the other group's O at the end, 32-bit: both arrays, 64 KB)
     unsigned char v[kStages][kTile];
     float m[kRows], l[kRows];                  // the second group's, at the end
-    unsigned long long q_full, full[kStages], free[kStages];   // K and V of a tile have landed; its products have been made
+    unsigned long long q_full, full[kStages];   // Q; K and V of a tile have landed
     unsigned long long s_full[2];              // S of a group's tile is in TMEM (and all products before it are done)
     unsigned long long p_ready[2];             // P of a group's tile is (128 arrivals)
     unsigned long long done;                   // every product
@@ -78,7 +78,6 @@ window_forward_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
         mbar_init(&sm.q_full, 1);
         for (int s = 0; s < kStages; ++s) {
             mbar_init(&sm.full[s], 1);
-            mbar_init(&sm.free[s], 1);
         }
         for (int w = 0; w < 2; ++w) {
             mbar_init(&sm.s_full[w], 1);
@@ -124,7 +123,12 @@ window_forward_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
             }
             for (; issued < n; ++issued) {
                 const int s = issued % kStages;
-                if (issued >= kStages && !mbar_wait(&sm.free[s], (issued / kStages - 1) & 1, limit, abort_flag, p.status)) break;
+                // (the place of tile j = issued - kStages is free with its group's next commit, the one of number j / 2 + 1)
+                const int j = issued - kStages;
+                // (a wait names a phase by its parity: the one before it has to be known to be over, so the first
+                // two tiles wait for commit 0 as well; commit j / 2 + 2 cannot come before tile j + 4 is here)
+                if (j >= 0 && j < 2 && !mbar_wait(&sm.s_full[j], 0, limit, abort_flag, p.status)) break;
+                if (j >= 0 && !mbar_wait(&sm.s_full[j & 1], ((j >> 1) + 1) & 1, limit, abort_flag, p.status)) break;
                 mbar_arrive_expect_tx(&sm.full[s], 2 * kTile);
                 tma_load_4d(sm.k[s], &tm_k, &sm.full[s], 0, hk, first_of(issued), b);
                 tma_load_4d(sm.v[s], &tm_v, &sm.full[s], 0, hk, first_of(issued), b);
@@ -148,38 +152,47 @@ window_forward_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
         constexpr uint64_t stage = kTile >> 4;
         const uint32_t minus = p.negate ? 1u << 13 : 0u;          // (the descriptor's negation of A)
         constexpr uint32_t idesc_pv = make_idesc(128, 64, 0, 1);  // P (tmem) x V (MN-major)
-        auto issue_s = [&](int i) {
+        // (the elected lane) S of tile i
+        auto scores = [&](int i) {
             const int s = i % kStages, w = i & 1;
-            if (!warp_wait(&sm.full[s], (i / kStages) & 1, limit, abort_flag, p.status)) return false;
+            const uint32_t idesc = make_idesc(128, 32 * blocks_of(i), 0, 0) | minus;
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk)
+                mma_ss(tmem + kColS + w * kGroupCols, dq + 2 * kk, dk + s * stage + 2 * kk, idesc, kk > 0);
+        };
+        auto landed = [&](int i) { return warp_wait(&sm.full[i % kStages], (i / kStages) & 1, limit, abort_flag, p.status); };
+        bool ok = n > 0 && warp_wait(&sm.q_full, 0, limit, abort_flag, p.status);
+        for (int i = 0; ok && i < min(n, 2); ++i) {
+            if (!(ok = landed(i))) break;
             tc_fence_after();
             if (elect_one()) {
-                const uint32_t idesc = make_idesc(128, 32 * blocks_of(i), 0, 0) | minus;
-#pragma unroll
-                for (int kk = 0; kk < 4; ++kk)
-                    mma_ss(tmem + kColS + w * kGroupCols, dq + 2 * kk, dk + s * stage + 2 * kk, idesc, kk > 0);
-                mma_commit(&sm.s_full[w]);
+                scores(i);
+                mma_commit(&sm.s_full[i]);
             }
             __syncwarp();
-            return true;
-        };
-        bool ok = n > 0 && warp_wait(&sm.q_full, 0, limit, abort_flag, p.status) && issue_s(0) && (n == 1 || issue_s(1));
+        }
         for (int i = 0; ok && i < n; ++i) {
             const int s = i % kStages, w = i & 1;
+            // (the wait for a tile that has most often landed long ago stands ahead of the one for P)
+            if (i + 2 < n && !(ok = landed(i + 2))) break;
             if (!(ok = warp_wait(&sm.p_ready[w], (i >> 1) & 1, limit, abort_flag, p.status))) break;
             tc_fence_after();
             if (elect_one()) {
                 const uint32_t at_p = tmem + kColS + w * kGroupCols, at_o = tmem + kColO + w * kGroupCols;
-                const int steps = 2 * blocks_of(i);
-#pragma unroll
-                for (int kk = 0; kk < 4; ++kk)           // 16 keys: 8 columns of P (keys 32-63 stand 32 on), 2048 bytes of V
-                    if (kk < steps)
-                        mma_ts(at_o, at_p + 32 * (kk >> 1) + 8 * (kk & 1), dv + s * stage + 128 * kk, idesc_pv, i > 1 || kk > 0);
-                mma_commit(&sm.free[s]);
+                const uint64_t at_v = dv + s * stage;
+                mma_ts(at_o, at_p, at_v, idesc_pv, i > 1);               // 16 keys: 8 columns of P, 2048 bytes of V
+                mma_ts(at_o, at_p + 8, at_v + 128, idesc_pv, 1);
+                if (blocks_of(i) > 1) {                                  // keys 32-63 stand 32 columns on
+                    mma_ts(at_o, at_p + 32, at_v + 256, idesc_pv, 1);
+                    mma_ts(at_o, at_p + 40, at_v + 384, idesc_pv, 1);
+                }
+                // the group's next S, over this P (the products run in the order they were issued); with
+                // it this tile's place is free
+                if (i + 2 < n) scores(i + 2);
+                mma_commit(&sm.s_full[w]);
                 if (i == n - 1) mma_commit(&sm.done);
             }
             __syncwarp();
-            // (over this tile's P: the products run in the order they were issued)
-            if (i + 2 < n) ok = issue_s(i + 2);
         }
         if (elect_one()) {
             mma_commit(&sm.drain);

@@ -42,7 +42,7 @@ struct Smem {
     unsigned char y1[kStages][kTile];
     unsigned char y2[kStages][kTile];
     float lse[2][2][kCols], delta[2][2][kCols];            // keys: of each group's tiles, by column, two in turn
-    unsigned long long full[kStages];                      // Y1 and Y2 have landed
+    unsigned long long full[kStages], free[kStages];       // Y1 and Y2 have landed; their products have been made
     unsigned long long x_ready;                            // X1 and X2 are in TMEM (2 kGroup arrivals)
     unsigned long long s_full[2];                          // S and dP of a group's tile are there (and all products before are done)
     unsigned long long p_ready[2];                         // P and dS are (kGroup arrivals)
@@ -98,7 +98,10 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
     const int b = bh / (KEYS ? p.Hk : p.Hq), h = bh - b * (KEYS ? p.Hk : p.Hq);
 
     if (tid == 0) {
-        for (int s = 0; s < kStages; ++s) mbar_init(&sm.full[s], 1);
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(&sm.full[s], 1);
+            mbar_init(&sm.free[s], 1);
+        }
         mbar_init(&sm.x_ready, 2 * kGroup);
         for (int w = 0; w < 2; ++w) {
             mbar_init(&sm.s_full[w], 1);
@@ -148,12 +151,7 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
             int issued = 0;
             for (; issued < n; ++issued) {
                 const int s = issued % kStages;
-                // (the place of tile j = issued - kStages is free with its group's next commit, the one of number j / 2 + 1)
-                const int j = issued - kStages;
-                // (a wait names a phase by its parity: the one before it has to be known to be over, so the first
-                // two tiles wait for commit 0 as well; commit j / 2 + 2 cannot come before tile j + 4 is here)
-                if (j >= 0 && j < 2 && !mbar_wait(&sm.s_full[j], 0, limit, abort_flag, p.status)) break;
-                if (j >= 0 && !mbar_wait(&sm.s_full[j & 1], ((j >> 1) + 1) & 1, limit, abort_flag, p.status)) break;
+                if (issued >= kStages && !mbar_wait(&sm.free[s], (issued / kStages - 1) & 1, limit, abort_flag, p.status)) break;
                 mbar_arrive_expect_tx(&sm.full[s], 2 * kTile);
                 tma_load_4d(sm.y1[s], &tm_y1, &sm.full[s], 0, head_of(issued), first_of(issued), b);
                 tma_load_4d(sm.y2[s], &tm_y2, &sm.full[s], 0, head_of(issued), first_of(issued), b);
@@ -205,10 +203,12 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
 #pragma unroll
                 for (int kk = 0; kk < 4; ++kk)
                     mma_ts(tmem + kColA1, at_ds + 32 * (kk >> 1) + 8 * (kk & 1), dy1 + s * stage + 128 * kk, idesc_a, i > 0 || kk > 0);
-                // the group's next S and dP, over this P and dS (the products run in the order they were
-                // issued); with them this tile's place is free
-                if (i + 2 < n) scores(i + 2);
-                mma_commit(&sm.s_full[w]);
+                mma_commit(&sm.free[s]);
+                // the group's next S and dP, over this P and dS (the products run in the order they were issued)
+                if (i + 2 < n) {
+                    scores(i + 2);
+                    mma_commit(&sm.s_full[w]);
+                }
                 if (i == n - 1) mma_commit(&sm.done);
             }
             __syncwarp();

@@ -338,7 +338,9 @@ window_forward_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
                 if (i == 0) {
                     m = top;
                 } else if (__any_sync(0xffffffffu, grow)) {
-                    const float now = grow ? top : m, f = grow ? ex2_approx(m - now) : 1.0f;
+                    // (every row of the warp moves to its maximum now, or its turn would come one by one: 25 % of
+                    // the steps scaled where only rows that had grown moved)
+                    const float now = fmaxf(m, top), f = now == m ? 1.0f : ex2_approx(m - now);
                     m = now;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) l[e] *= f;

@@ -420,10 +420,9 @@ int lasad_window_attention_backward(lasad_ctx* ctx, const lasad_window_params* p
  * earlier tokens have filled must hold them.  The call writes k and v to the token's slot.  A
  * negative position is a sequence that takes no part: its o is 0 and its cache is not touched.
  */
-int64_t lasad_window_attention_step_workspace(lasad_ctx* ctx, const lasad_window_params* p);
 int lasad_window_attention_step(lasad_ctx* ctx, const lasad_window_params* p, const void* q, const void* k,
                                 const void* v, void* k_cache, void* v_cache, const int32_t* pos, void* o,
-                                void* workspace, void* cuda_stream);
+                                void* cuda_stream);
 /* Puts the keys and values of a prefill, k, v [B,T,Hk,d] (tokens 0 to lengths[b] - 1, or T - 1), into
  * such caches; slots that no token has reached are not written. */
 int lasad_window_cache_store(lasad_ctx* ctx, const lasad_window_params* p, const void* k, const void* v,

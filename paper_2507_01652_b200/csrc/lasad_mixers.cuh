@@ -159,9 +159,7 @@ cudaError_t launch_window_forward_tc(const WindowArgs& a, cudaStream_t st);     
 cudaError_t launch_window_backward_tc(const WindowArgs& a, cudaStream_t st);     // two launches, behind launch_window_prep
 cudaError_t launch_window_forward_simt(const WindowArgs& a, cudaStream_t st);
 cudaError_t launch_window_backward_simt(const WindowArgs& a, cudaStream_t st);   // two launches, behind launch_window_prep
-// One token against the ring cache.  splits: CTAs along the slots (window_step_splits).
-int window_step_splits(const WindowArgs& a);
-size_t window_step_workspace_bytes(const WindowArgs& a);
+// One token against the ring cache.
 cudaError_t launch_window_step(const WindowArgs& a, cudaStream_t st);
 cudaError_t launch_window_store(const WindowArgs& a, cudaStream_t st);
 

@@ -309,27 +309,17 @@ int lasad_window_attention_backward(lasad_ctx* ctx, const lasad_window_params* p
     return launched(ctx, e, 3);
 }
 
-int64_t lasad_window_attention_step_workspace(lasad_ctx* ctx, const lasad_window_params* p)
-{
-    lasad::WindowArgs a{};
-    const int rc = window_args(ctx, p, kStep, a);
-    return rc != LASAD_OK ? rc : (int64_t)lasad::window_step_workspace_bytes(a);
-}
-
 int lasad_window_attention_step(lasad_ctx* ctx, const lasad_window_params* p, const void* q, const void* k,
                                 const void* v, void* k_cache, void* v_cache, const int32_t* pos, void* o,
-                                void* workspace, void* cuda_stream)
+                                void* cuda_stream)
 {
     lasad::WindowArgs a{};
     const int rc = window_args(ctx, p, kStep, a);
     if (rc != LASAD_OK) return rc;
-    if (!q || !k || !v || !k_cache || !v_cache || !pos || !o || (!workspace && lasad::window_step_workspace_bytes(a)))
-        return LASAD_ERR_INVALID_ARG;
-    if (!all16({q, k, v, k_cache, v_cache, o, workspace}) || !aligned(pos, 4)) return LASAD_ERR_INVALID_ARG;
+    if (!q || !k || !v || !k_cache || !v_cache || !pos || !o) return LASAD_ERR_INVALID_ARG;
+    if (!all16({q, k, v, k_cache, v_cache, o}) || !aligned(pos, 4)) return LASAD_ERR_INVALID_ARG;
     a.q = q, a.k = k, a.v = v, a.kc = k_cache, a.vc = v_cache, a.pos = pos, a.o = o;
-    a.ws = static_cast<float*>(workspace);
-    return launched(ctx, lasad::launch_window_step(a, static_cast<cudaStream_t>(cuda_stream)),
-                    lasad::window_step_splits(a) > 1 ? 2 : 1);
+    return launched(ctx, lasad::launch_window_step(a, static_cast<cudaStream_t>(cuda_stream)), 1);
 }
 
 int lasad_window_cache_store(lasad_ctx* ctx, const lasad_window_params* p, const void* k, const void* v,

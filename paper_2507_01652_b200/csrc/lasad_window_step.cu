@@ -8,15 +8,19 @@
 // Bound by reading the cache once.  A key row lies in the 16-byte pieces of d / 8 (bf16) or d / 4
 // (fp32) lanes; all query heads that share the key head (up to eight at a time) work on the row
 // while it is in registers.  Every group of lanes keeps its own running maximum and sum over its
-// rows; they are joined once, by shuffles, shared memory, and, where few sequences leave SMs idle
-// and the slots are cut over several CTAs, by the last CTA of a (sequence, key head) to finish.
+// rows; they are joined once, by shuffles, and, where several warps have a (sequence, key head), in
+// shared memory.  Who has one goes by how many there are: with 16 and more per SM a warp each (nothing
+// is shared, and a CTA's warps are independent: 256 x 20 of 65 slots 17 us, with a CTA each 27 us); with
+// fewer a CTA of eight warps each, and with fewer than SMs a cluster of up to eight CTAs, whose parts the
+// first one joins.
 #include "lasad_mixers.cuh"
 #include "lasad_tc_ptx.cuh"
 
 namespace lasad {
 namespace {
 
-constexpr int kStepWarps = 4;
+constexpr int kStepWarps = 8, kMaxCluster = 8;      // of a CTA that has one unit; of a unit
+constexpr int kSoloWarps = 4, kSoloCtas = 6;        // of a CTA whose warps have a unit each; on an SM
 constexpr float kLog2e = 1.4426950408889634f;
 
 template <typename T> struct row_piece;
@@ -28,6 +32,10 @@ template <> struct row_piece<__nv_bfloat16> {
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[2 * i] = tcx::bf16_lo(w[i]), v[2 * i + 1] = tcx::bf16_hi(w[i]);
     }
+    static __device__ __forceinline__ uint4 put(const float (&v)[8])
+    {
+        return make_uint4(tcx::pack_bf16(v[0], v[1]), tcx::pack_bf16(v[2], v[3]), tcx::pack_bf16(v[4], v[5]), tcx::pack_bf16(v[6], v[7]));
+    }
 };
 template <> struct row_piece<float> {
     static constexpr int N = 4;
@@ -35,38 +43,65 @@ template <> struct row_piece<float> {
     {
         v[0] = __uint_as_float(r.x), v[1] = __uint_as_float(r.y), v[2] = __uint_as_float(r.z), v[3] = __uint_as_float(r.w);
     }
+    static __device__ __forceinline__ uint4 put(const float (&v)[4])
+    {
+        return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    }
 };
+
+template <int V> struct Int { static constexpr int value = V; };
+
+// Reads the same place of the shared memory of the cluster's CTA number `rank`.
+__device__ __forceinline__ float of_rank(const float* p, int rank)
+{
+    float x;
+    asm volatile("{\n\t.reg .b32 r;\n\tmapa.shared::cluster.u32 r, %1, %2;\n\tld.shared::cluster.f32 %0, [r];\n\t}"
+                 : "=f"(x)
+                 : "r"(tcx::smem_u32(p)), "r"(rank)
+                 : "memory");
+    return x;
+}
 
 // Joins (m2, l2, o2) into (m, l, o): the same softmax over two sets of rows.  Maxima are in powers of two.
 template <int N>
 __device__ __forceinline__ void join(float& m, float& l, float (&o)[N], float m2, float l2, const float (&o2)[N])
 {
     const float top = fmaxf(m, m2), base = top == -INFINITY ? 0.0f : top;
-    const float f = exp2f(m - base), f2 = exp2f(m2 - base);
+    const float f = tcx::ex2_approx(m - base), f2 = tcx::ex2_approx(m2 - base);
     m = top;
     l = l * f + l2 * f2;
 #pragma unroll
     for (int e = 0; e < N; ++e) o[e] = o[e] * f + o2[e] * f2;
 }
 
-// grid: (splits, Hk * head chunks, B).  GB: query heads of one CTA.
-template <typename T, int D, int GB>
-__global__ void __launch_bounds__(32 * kStepWarps) window_step_kernel(const WindowArgs a, int per_split)
+// Accesses of a warp in flight, per tensor (and as many of the next rows): what the registers of GB
+// query heads leave room for, with many warps on an SM (SOLO) or eight.
+template <int GB, bool SOLO> struct ahead { static constexpr int value = SOLO ? (GB == 1 ? 3 : GB <= 4 ? 2 : 1) : GB == 1 ? 6 : GB <= 3 ? 4 : GB == 4 ? 3 : GB == 6 ? 2 : 1; };
+
+// A unit is a sequence, a key head and up to GB of its query heads.  SOLO: a warp has a unit; else a CTA
+// has one, or its cluster (blockIdx.x = unit * cluster + rank) with per_cta slots for each CTA.
+template <typename T, int D, int GB, bool SOLO>
+__global__ void __launch_bounds__(32 * (SOLO ? kSoloWarps : kStepWarps), SOLO && GB == 1 ? kSoloCtas : 1) window_step_kernel(const WindowArgs a, int cluster, int per_cta)
 {
     typedef row_piece<T> P;
-    constexpr int N = P::N, LANES = D / N, ROWS = 32 / LANES, AHEAD = 4;   // rows of one access of a warp; accesses in flight
-    __shared__ float part[kStepWarps][GB][D + 2];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane % LANES, mine = lane / LANES;
-    const int G = a.Hq / a.Hk, hchunks = (G + GB - 1) / GB;
-    const int hk = blockIdx.y / hchunks, g0 = (blockIdx.y - hk * hchunks) * GB, b = blockIdx.z;
-    const int heads = min(GB, G - g0), h0 = hk * G + g0;
+    constexpr int N = P::N, LANES = D / N, ROWS = 32 / LANES, AHEAD = ahead<GB, SOLO>::value;   // ROWS: of one access of a warp
+    constexpr int WARPS = SOLO ? 1 : kStepWarps;                                          // warps of a unit in this CTA
+    __shared__ float part[SOLO ? 1 : kStepWarps][GB][D + 2];
+    __shared__ float whole[GB][D + 2];                               // the CTA's part of its cluster's result
+    const int lane = threadIdx.x & 31, warp = SOLO ? 0 : threadIdx.x >> 5, sub = lane % LANES, mine = lane / LANES;
+    const int G = a.Hq / a.Hk, hchunks = (G + GB - 1) / GB, per_b = a.Hk * hchunks;
+    const int unit = SOLO ? blockIdx.x * kSoloWarps + (threadIdx.x >> 5) : blockIdx.x / cluster;
+    const int rank = SOLO ? 0 : blockIdx.x - unit * cluster;
     pdl_wait();
+    if (SOLO && unit >= a.B * per_b) return;
+    const int b = unit / per_b, y = unit - b * per_b, hk = y / hchunks, g0 = (y - hk * hchunks) * GB;
+    const int heads = min(GB, G - g0), h0 = hk * G + g0;
     const int pos = a.pos[b];
     const int S = a.sinks, W = a.window;
     // slots in use, 0 .. n - 1, and the token's own
     const int n = pos < 0 ? 0 : pos < S + W ? pos + 1 : S + W;
     const int own = pos < S ? pos : S + (pos - S) % W;
-    const int lo = blockIdx.x * per_split, hi = min(lo + per_split, n);
+    const int lo = SOLO ? 0 : rank * per_cta, hi = SOLO ? n : min(lo + per_cta, n);
     const T* knew = static_cast<const T*>(a.k) + b * a.ks[0] + hk * a.ks[2] + sub * N;
     const T* vnew = static_cast<const T*>(a.v) + b * a.vs[0] + hk * a.vs[2] + sub * N;
     T* kc = static_cast<T*>(a.kc) + b * a.kcs[0] + hk * a.kcs[2] + sub * N;
@@ -81,27 +116,13 @@ __global__ void __launch_bounds__(32 * kStepWarps) window_step_kernel(const Wind
 #pragma unroll
         for (int e = 0; e < N; ++e) q[g][e] *= a.scale * kLog2e, o[g][e] = 0.0f;
     }
-    for (int r0 = lo; r0 < hi; r0 += kStepWarps * ROWS * AHEAD) {
-        uint4 rk[AHEAD], rv[AHEAD];
-        bool live[AHEAD];
+    // n accesses' rows: a dot product per query head, the running maximum once, then the values
+    auto take = [&](auto& rk, auto& rv, int first, int end, int skip, auto count) {
+        constexpr int C = decltype(count)::value;
+        float x[C][GB];
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-            const int r = r0 + (i * kStepWarps + warp) * ROWS + mine;
-            live[i] = r < hi;
-            rk[i] = rv[i] = make_uint4(0, 0, 0, 0);
-            if (live[i]) {
-                const bool fresh = r == own;         // (its slot may not hold it yet)
-                rk[i] = *reinterpret_cast<const uint4*>(fresh ? knew : kc + r * a.kcs[1]);
-                rv[i] = *reinterpret_cast<const uint4*>(fresh ? vnew : vc + r * a.vcs[1]);
-                if (fresh && g0 == 0) {
-                    *reinterpret_cast<uint4*>(kc + r * a.kcs[1]) = rk[i];
-                    *reinterpret_cast<uint4*>(vc + r * a.vcs[1]) = rv[i];
-                }
-            }
-        }
-        float x[AHEAD][GB];
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
+        for (int i = 0; i < C; ++i) {
+            const bool live = first + i * WARPS * ROWS < end && first + i * WARPS * ROWS != skip;
             float k[N];
             P::get(rk[i], k);
 #pragma unroll
@@ -111,27 +132,27 @@ __global__ void __launch_bounds__(32 * kStepWarps) window_step_kernel(const Wind
                 for (int e = 0; e < N; ++e) s = fmaf(q[g][e], k[e], s);
 #pragma unroll
                 for (int w = LANES / 2; w >= 1; w >>= 1) s += __shfl_xor_sync(0xffffffffu, s, w);
-                x[i][g] = live[i] ? s : -INFINITY;
+                x[i][g] = live ? s : -INFINITY;
             }
         }
 #pragma unroll
         for (int g = 0; g < GB; ++g) {
             float top = m[g];
 #pragma unroll
-            for (int i = 0; i < AHEAD; ++i) top = fmaxf(top, x[i][g]);
-            const float base = top == -INFINITY ? 0.0f : top, keep = exp2f(m[g] - base);
+            for (int i = 0; i < C; ++i) top = fmaxf(top, x[i][g]);
+            const float base = top == -INFINITY ? 0.0f : top, keep = tcx::ex2_approx(m[g] - base);
             m[g] = top;
             l[g] *= keep;
 #pragma unroll
             for (int e = 0; e < N; ++e) o[g][e] *= keep;
 #pragma unroll
-            for (int i = 0; i < AHEAD; ++i) {
-                x[i][g] = exp2f(x[i][g] - base);
+            for (int i = 0; i < C; ++i) {
+                x[i][g] = tcx::ex2_approx(x[i][g] - base);
                 l[g] += x[i][g];
             }
         }
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
+        for (int i = 0; i < C; ++i) {
             float v[N];
             P::get(rv[i], v);
 #pragma unroll
@@ -139,8 +160,45 @@ __global__ void __launch_bounds__(32 * kStepWarps) window_step_kernel(const Wind
 #pragma unroll
                 for (int e = 0; e < N; ++e) o[g][e] = fmaf(x[i][g], v[e], o[g][e]);
         }
+    };
+    // rows first, first + WARPS * ROWS, ..; the token's own slot may not hold it yet: it comes by itself
+    const long long kstep = WARPS * ROWS * a.kcs[1], vstep = WARPS * ROWS * a.vcs[1];
+    int row = lo + warp * ROWS + mine;
+    const T* kp = kc + row * a.kcs[1];
+    const T* vp = vc + row * a.vcs[1];
+    auto load = [&](uint4 (&tk)[AHEAD], uint4 (&tv)[AHEAD], int first) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i, kp += kstep, vp += vstep) {
+            const int r = first + i * WARPS * ROWS;
+            tk[i] = tv[i] = make_uint4(0, 0, 0, 0);
+            if (r < hi && r != own) {
+                tk[i] = *reinterpret_cast<const uint4*>(kp);
+                tv[i] = *reinterpret_cast<const uint4*>(vp);
+            }
+        }
+    };
+    constexpr int STEP = WARPS * ROWS * AHEAD;
+    uint4 rk[2][AHEAD], rv[2][AHEAD];
+    load(rk[0], rv[0], row);
+    if (own >= lo && own < hi && warp == 0) {        // (uniform over the warp)
+        uint4 ok[1] = {make_uint4(0, 0, 0, 0)}, ov[1] = {make_uint4(0, 0, 0, 0)};
+        if (mine == 0) {
+            ok[0] = *reinterpret_cast<const uint4*>(knew);
+            ov[0] = *reinterpret_cast<const uint4*>(vnew);
+            if (g0 == 0) {
+                *reinterpret_cast<uint4*>(kc + own * a.kcs[1]) = ok[0];
+                *reinterpret_cast<uint4*>(vc + own * a.vcs[1]) = ov[0];
+            }
+        }
+        take(ok, ov, mine, 1, -1, Int<1>());       // (lane group 0 alone)
     }
-    // the groups of lanes of the warp, then the warps
+    for (int r0 = lo; r0 < hi; r0 += 2 * STEP, row += 2 * STEP) {     // (uniform; the next rows come in under these ones' arithmetic)
+        load(rk[1], rv[1], row + STEP);
+        take(rk[0], rv[0], row, hi, own, Int<AHEAD>());
+        load(rk[0], rv[0], row + 2 * STEP);
+        if (r0 + STEP < hi) take(rk[1], rv[1], row + STEP, hi, own, Int<AHEAD>());
+    }
+    // the groups of lanes of the warp
 #pragma unroll
     for (int g = 0; g < GB; ++g) {
 #pragma unroll
@@ -152,12 +210,25 @@ __global__ void __launch_bounds__(32 * kStepWarps) window_step_kernel(const Wind
             join<N>(m[g], l[g], o[g], m2, l2, o2);
         }
         if (mine == 0) {
+            if (SOLO) {
+                if (g < heads) {
+                    const float inv = l[g] > 0.0f || l[g] != l[g] ? 1.0f / l[g] : 0.0f;
+                    T* out = static_cast<T*>(a.o) + b * a.os[0] + (h0 + g) * a.os[2] + sub * N;
+                    float r[N];
 #pragma unroll
-            for (int e = 0; e < N; ++e) part[warp][g][sub * N + e] = o[g][e];
-            if (sub == 0) part[warp][g][D] = m[g], part[warp][g][D + 1] = l[g];
+                    for (int e = 0; e < N; ++e) r[e] = o[g][e] * inv;
+                    *reinterpret_cast<uint4*>(out) = P::put(r);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; ++e) part[warp][g][sub * N + e] = o[g][e];
+                if (sub == 0) part[warp][g][D] = m[g], part[warp][g][D + 1] = l[g];
+            }
         }
     }
+    if (SOLO) return;
     __syncthreads();
+    // the warps of the CTA
     for (int i = threadIdx.x; i < heads * D; i += 32 * kStepWarps) {
         const int g = i / D, c = i - g * D;
         float mm = -INFINITY, ll = 0.0f, oo[1] = {0.0f};
@@ -166,45 +237,31 @@ __global__ void __launch_bounds__(32 * kStepWarps) window_step_kernel(const Wind
             const float o2[1] = {part[w][g][c]};
             join<1>(mm, ll, oo, part[w][g][D], part[w][g][D + 1], o2);
         }
-        if (gridDim.x == 1) {
-            const float v = ll > 0.0f || ll != ll ? oo[0] / ll : 0.0f;
-            io<T>::store(static_cast<T*>(a.o) + b * a.os[0] + (h0 + g) * a.os[2] + c, v);
+        if (cluster == 1) {
+            io<T>::store(static_cast<T*>(a.o) + b * a.os[0] + (h0 + g) * a.os[2] + c, ll > 0.0f || ll != ll ? oo[0] / ll : 0.0f);
         } else {
-            float* w = a.ws + (((long long)b * a.Hq + h0 + g) * gridDim.x + blockIdx.x) * (D + 2);
-            w[c] = oo[0];
-            if (c == 0) w[D] = mm, w[D + 1] = ll;
+            whole[g][c] = oo[0];
+            if (c == 0) whole[g][D] = mm, whole[g][D + 1] = ll;
         }
     }
-}
-
-// Joins the splits' parts: one warp per (sequence, head).
-template <typename T, int D>
-__global__ void __launch_bounds__(128) window_step_join_kernel(const WindowArgs a, int splits)
-{
-    pdl_wait();
-    const int row = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    if (row >= a.B * a.Hq) return;
-    const int b = row / a.Hq, h = row - b * a.Hq;
-    const float* w = a.ws + (long long)row * splits * (D + 2);
-    float top = -INFINITY;
-    for (int s = lane; s < splits; s += 32) top = fmaxf(top, w[s * (D + 2) + D]);
+    if (cluster == 1) return;
+    // the CTAs of the cluster, by the first one; the others stay until it has read their parts
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (rank == 0)
+        for (int i = threadIdx.x; i < heads * D; i += 32 * kStepWarps) {
+            const int g = i / D, c = i - g * D;
+            float m2[kMaxCluster], l2[kMaxCluster], o2[kMaxCluster][1];    // (all asked for before the first is used)
 #pragma unroll
-    for (int o = 16; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const float base = top == -INFINITY ? 0.0f : top;
-    float l = 0.0f, o[D / 32];
+            for (int w = 0; w < kMaxCluster; ++w) {
+                m2[w] = -INFINITY, l2[w] = o2[w][0] = 0.0f;
+                if (w < cluster) m2[w] = of_rank(&whole[g][D], w), l2[w] = of_rank(&whole[g][D + 1], w), o2[w][0] = of_rank(&whole[g][c], w);
+            }
+            float mm = -INFINITY, ll = 0.0f, oo[1] = {0.0f};
 #pragma unroll
-    for (int e = 0; e < D / 32; ++e) o[e] = 0.0f;
-#pragma unroll 4
-    for (int s = 0; s < splits; ++s) {
-        const float* p = w + s * (D + 2);
-        const float f = exp2f(p[D] - base);
-        l = fmaf(p[D + 1], f, l);
-#pragma unroll
-        for (int e = 0; e < D / 32; ++e) o[e] = fmaf(p[lane + 32 * e], f, o[e]);
-    }
-#pragma unroll
-    for (int e = 0; e < D / 32; ++e)
-        io<T>::store(static_cast<T*>(a.o) + b * a.os[0] + h * a.os[2] + lane + 32 * e, l > 0.0f || l != l ? o[e] / l : 0.0f);
+            for (int w = 0; w < kMaxCluster; ++w) join<1>(mm, ll, oo, m2[w], l2[w], o2[w]);
+            io<T>::store(static_cast<T*>(a.o) + b * a.os[0] + (h0 + g) * a.os[2] + c, ll > 0.0f || ll != ll ? oo[0] / ll : 0.0f);
+        }
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 // The prefill's keys and values into the ring: slot n gets the last token of the sequence that
@@ -228,45 +285,49 @@ __global__ void __launch_bounds__(256) window_store_kernel(const WindowArgs a)
         *reinterpret_cast<const uint4*>(static_cast<const T*>(a.v) + b * a.vs[0] + t * a.vs[1] + h * a.vs[2] + c);
 }
 
-// Query heads of one CTA: the group that shares a key head, up to eight.
-int heads_per_cta(const WindowArgs& a)
+template <typename T, int D, int GB>
+cudaError_t step_g(const WindowArgs& a, cudaStream_t st)
 {
     const int G = a.Hq / a.Hk;
-    return G == 1 ? 1 : G == 2 ? 2 : G <= 4 ? 4 : 8;
+    const long long units = (long long)a.B * a.Hk * ((G + GB - 1) / GB), slots = a.sinks + (long long)a.window;
+    if (units >= 16LL * a.sms)
+        return launch_dependent(window_step_kernel<T, D, GB, true>, dim3((unsigned)((units + kSoloWarps - 1) / kSoloWarps)),
+                                dim3(32 * kSoloWarps), 0, st, a, 1, 0);
+    // CTAs of a unit: as long as the SMs have room and a CTA keeps 64 slots
+    int cluster = 1;
+    while (cluster < kMaxCluster && units * cluster * 2 <= a.sms && slots >= 128LL * cluster) cluster *= 2;
+    const int per = (int)((slots + cluster - 1) / cluster);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(units * cluster));
+    cfg.blockDim = dim3(32 * kStepWarps);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, window_step_kernel<T, D, GB, false>, a, cluster, per);
 }
-
 template <typename T, int D>
 cudaError_t step_t(const WindowArgs& a, cudaStream_t st)
 {
-    const int GB = heads_per_cta(a), G = a.Hq / a.Hk, splits = window_step_splits(a);
-    const long long slots = a.sinks + (long long)a.window;
-    const int per = (int)((slots + splits - 1) / splits);
-    const dim3 grid(splits, a.Hk * ((G + GB - 1) / GB), a.B);
-    auto kernel = GB == 1 ? window_step_kernel<T, D, 1> : GB == 2 ? window_step_kernel<T, D, 2>
-                : GB == 4 ? window_step_kernel<T, D, 4> : window_step_kernel<T, D, 8>;
-    const cudaError_t e = launch_dependent(kernel, grid, dim3(32 * kStepWarps), 0, st, a, per);
-    if (e != cudaSuccess || splits == 1) return e;
-    return launch_dependent(window_step_join_kernel<T, D>, dim3((unsigned)((a.B * a.Hq + 3) / 4)), dim3(128), 0, st, a, splits);
+    // query heads of one unit: the group that shares a key head, up to eight
+    const int G = a.Hq / a.Hk;
+    switch (G) {
+        case 1: return step_g<T, D, 1>(a, st);
+        case 2: return step_g<T, D, 2>(a, st);
+        case 3: return step_g<T, D, 3>(a, st);
+        case 4: return step_g<T, D, 4>(a, st);
+        case 5:
+        case 6: return step_g<T, D, 6>(a, st);
+        default: return step_g<T, D, 8>(a, st);
+    }
 }
 
 }  // namespace
-
-int window_step_splits(const WindowArgs& a)
-{
-    const int GB = heads_per_cta(a), G = a.Hq / a.Hk;
-    const long long ctas = (long long)a.B * a.Hk * ((G + GB - 1) / GB), slots = a.sinks + (long long)a.window;
-    long long splits = (4LL * a.sms + ctas - 1) / ctas;
-    const long long most = (slots + 63) / 64;
-    if (splits > most) splits = most;
-    if (splits < 1) splits = 1;
-    const long long per = (slots + splits - 1) / splits;
-    return (int)((slots + per - 1) / per);
-}
-size_t window_step_workspace_bytes(const WindowArgs& a)
-{
-    const int splits = window_step_splits(a);
-    return splits == 1 ? 0 : (size_t)a.B * a.Hq * splits * (a.d + 2) * sizeof(float);
-}
 
 cudaError_t launch_window_step(const WindowArgs& a, cudaStream_t st)
 {

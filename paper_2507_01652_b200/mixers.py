@@ -59,8 +59,7 @@ PROTOTYPES = {
     "lasad_window_attention": (ctypes.c_int, [_VP, _WP] + [_VP] * 7),
     "lasad_window_attention_workspace": (_I64, [_VP, _WP]),
     "lasad_window_attention_backward": (ctypes.c_int, [_VP, _WP] + [_VP] * 12),
-    "lasad_window_attention_step_workspace": (_I64, [_VP, _WP]),
-    "lasad_window_attention_step": (ctypes.c_int, [_VP, _WP] + [_VP] * 9),
+    "lasad_window_attention_step": (ctypes.c_int, [_VP, _WP] + [_VP] * 8),
     "lasad_window_cache_store": (ctypes.c_int, [_VP, _WP] + [_VP] * 6),
 }
 
@@ -376,7 +375,7 @@ class Mixers:
         return dq, dk, dv
 
     def lasad_window_attention_step(self, q, k, v, k_cache, v_cache, pos, window, sinks=0, scale=None, o=None,
-                                    workspace=None, stream=None):
+                                    stream=None):
         """One new token per sequence, q [B,Hq,d], k, v [B,Hk,d], against ring caches [B, sinks +
         window, Hk, d], which get the token's k and v.  ``pos`` int32 [B]: the tokens' positions
         (negative: the sequence takes no part).  Returns o [B,Hq,d]."""
@@ -392,10 +391,8 @@ class Mixers:
                              v_cache=v_cache)
         p = e.p
         p.scale = 1.0 / math.sqrt(p.d) if scale is None else scale
-        ws = self._workspace(e, self._lib.lasad_window_attention_step_workspace, q, workspace, stream)
         rc = self._lib.lasad_window_attention_step(self._h, e.ref, q.data_ptr(), k.data_ptr(), v.data_ptr(), k_cache.data_ptr(),
-                                                   v_cache.data_ptr(), pos.data_ptr(), o.data_ptr(), _ptr(ws),
-                                                   _stream(q.device, stream))
+                                                   v_cache.data_ptr(), pos.data_ptr(), o.data_ptr(), _stream(q.device, stream))
         if rc:
             self._raise(rc, "lasad_window_attention_step")
         return o

@@ -380,6 +380,8 @@ def test_window_long_ragged_against_the_other_implementation_and_repeats(ctx, dt
 STEP = [  # B, Hq, Hk, d, window, sinks
     (1, 1, 1, 64, 1, 0), (3, 2, 1, 64, 5, 0), (4, 3, 3, 32, 16, 2), (2, 8, 1, 64, 200, 1), (5, 12, 4, 64, 64, 1),
     (2, 10, 1, 64, 33, 3), (1, 24, 8, 64, 1500, 1), (40, 4, 4, 64, 70, 4),
+    # so many heads that each has one warp; few, with clusters of CTAs along the slots
+    (130, 20, 20, 64, 6, 1), (400, 18, 6, 32, 9, 0), (700, 40, 4, 64, 3, 1), (2, 4, 2, 32, 3000, 2), (3, 16, 2, 64, 700, 0),
 ]
 
 

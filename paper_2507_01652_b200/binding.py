@@ -152,6 +152,7 @@ class Lasad(_mixers.Mixers):
         if rc != LASAD_OK:
             raise LasadError(rc, "lasad_create")
         self._h = h
+        self._calls = {}
 
     def close(self):
         if getattr(self, "_h", None):

@@ -75,9 +75,7 @@ def rope_table(rows: int, d: int, grid: bool, base: float = 10000.0, device=None
 # What a call looks like: the shape, strides, type and place of every tensor, or None.  A call that
 # looks like one before it has been checked and has its params struct and workspace size already
 # (checking and building them costs more than the rest of the call); scalars are set again each time.
-_cache = {}
-
-
+# A context keeps its own (``_calls``): like the context, they serve one host thread at a time.
 def _look(t):
     return None if t is None else (t.shape, t.stride(), t.dtype, t.is_cuda)
 
@@ -92,13 +90,6 @@ class _Entry:
 
     def __init__(self, p):
         self.p, self.ref, self.ws = p, ctypes.byref(p), None
-
-
-def _new(key, p):
-    if len(_cache) > 256:
-        _cache.clear()
-    e = _cache[key] = _Entry(p)
-    return e
 
 
 def _same(what, *ts):
@@ -134,6 +125,12 @@ def _strides2(t):
 class Mixers:
     """The calls beside LASAD; a base of ``binding.Lasad``, which has the library and the context."""
 
+    def _new(self, key, p):
+        if len(self._calls) > 256:
+            self._calls.clear()
+        e = self._calls[key] = _Entry(p)
+        return e
+
     def _workspace(self, e, query, like, given, stream):
         if e.ws is None:
             n = query(self._h, e.ref)
@@ -165,7 +162,7 @@ class Mixers:
             _f32(name, t, (B, C))
         _f32("saved", saved, (B, -(-T // LASAD_SCAN_CHUNK), C))
         _i32("pos", pos, B)
-        return _new(key, ScanParams(B, T, C, 0, 0, _dtype_code(x), 0, 0, 0, *[_strides2(t) for t in (x, gate, y, dx, dgate)]))
+        return self._new(key, ScanParams(B, T, C, 0, 0, _dtype_code(x), 0, 0, 0, *[_strides2(t) for t in (x, gate, y, dx, dgate)]))
 
     @staticmethod
     def _scan_set(p, grid_w, prefix_len, t0, tied, logits):
@@ -179,8 +176,8 @@ class Mixers:
         ``save`` keeps the states that ``lasad_scan_backward`` needs."""
         if y is None:
             y = _like(x)
-        key = ("scan", self.device, _look(x), _look(gate), _look(h_in), _look(y), _look(h_out))
-        e = _cache.get(key) or self._scan(key, "forward", x, gate, y, None, None, (("h_in", h_in), ("h_out", h_out)), None, None)
+        key = ("scan", _look(x), _look(gate), _look(h_in), _look(y), _look(h_out))
+        e = self._calls.get(key) or self._scan(key, "forward", x, gate, y, None, None, (("h_in", h_in), ("h_out", h_out)), None, None)
         p = e.p
         self._scan_set(p, grid_w, prefix_len, t0, tied, logits)
         if h_out is None and want_state:
@@ -200,9 +197,9 @@ class Mixers:
             dx = _like(x)
         if dgate is None:
             dgate = _like(x)
-        key = ("scan'", self.device, _look(x), _look(gate), _look(saved), _look(dy), _look(dh_out), _look(dx), _look(dgate),
+        key = ("scan'", _look(x), _look(gate), _look(saved), _look(dy), _look(dh_out), _look(dx), _look(dgate),
                _look(dh_in))
-        e = _cache.get(key)
+        e = self._calls.get(key)
         if e is None:
             if saved is None:
                 raise ValueError("saved is what lasad_scan_forward returns with save=True")
@@ -227,8 +224,8 @@ class Mixers:
             y = _like(x)
         if h_out is None:
             h_out = h_in
-        key = ("scan1", self.device, _look(x), _look(gate), _look(h_in), _look(y), _look(h_out), _look(pos))
-        e = _cache.get(key) or self._scan(key, "step", x, gate, y, None, None, (("h_in", h_in), ("h_out", h_out)), None, pos)
+        key = ("scan1", _look(x), _look(gate), _look(h_in), _look(y), _look(h_out), _look(pos))
+        e = self._calls.get(key) or self._scan(key, "step", x, gate, y, None, None, (("h_in", h_in), ("h_out", h_out)), None, pos)
         self._scan_set(e.p, grid_w, prefix_len, t, tied, logits)
         rc = self._lib.lasad_scan_step(self._h, e.ref, x.data_ptr(), gate.data_ptr(), h_in.data_ptr(), y.data_ptr(),
                                        h_out.data_ptr(), _ptr(pos), _stream(x.device, stream))
@@ -252,7 +249,7 @@ class Mixers:
         _f32("q_weight", q_weight, (d,))
         _f32("k_weight", k_weight, (d,))
         _i32("pos", pos, B)
-        return _new(key, RopeParams(B, T, Hq, k.shape[2], d, _dtype_code(q), 0, 0, table.shape[0], 0, 0.0, 0, 0, _strides3(q),
+        return self._new(key, RopeParams(B, T, Hq, k.shape[2], d, _dtype_code(q), 0, 0, table.shape[0], 0, 0.0, 0, 0, _strides3(q),
                                     _strides3(k), *[(_I64 * 3)() if t is None else _strides3(t) for t in outs]))
 
     @staticmethod
@@ -267,9 +264,9 @@ class Mixers:
             q_out = _like(q)
         if k_out is None:
             k_out = _like(k)
-        key = ("rope", self.device, grid_w > 0, _look(q), _look(k), _look(table), _look(q_weight), _look(k_weight), _look(pos),
+        key = ("rope", grid_w > 0, _look(q), _look(k), _look(table), _look(q_weight), _look(k_weight), _look(pos),
                _look(q_out), _look(k_out))
-        e = _cache.get(key) or self._rope(key, q, k, table, q_weight, k_weight, pos, grid_w > 0,
+        e = self._calls.get(key) or self._rope(key, q, k, table, q_weight, k_weight, pos, grid_w > 0,
                                           (q_out, k_out, None, None, None, None))
         self._rope_set(e.p, grid_w, prefix_len, t0, half, eps)
         rc = self._lib.lasad_qk_norm_rope(self._h, e.ref, q.data_ptr(), k.data_ptr(), table.data_ptr(), _ptr(q_weight),
@@ -287,9 +284,9 @@ class Mixers:
             dq = _like(q)
         if dk is None:
             dk = _like(k)
-        key = ("rope'", self.device, grid_w > 0, _look(q), _look(k), _look(table), _look(q_weight), _look(k_weight), _look(pos),
+        key = ("rope'", grid_w > 0, _look(q), _look(k), _look(table), _look(q_weight), _look(k_weight), _look(pos),
                _look(dq_out), _look(dk_out), _look(dq), _look(dk))
-        e = _cache.get(key) or self._rope(key, q, k, table, q_weight, k_weight, pos, grid_w > 0,
+        e = self._calls.get(key) or self._rope(key, q, k, table, q_weight, k_weight, pos, grid_w > 0,
                                           (None, None, dq_out, dk_out, dq, dk))
         self._rope_set(e.p, grid_w, prefix_len, t0, half, eps)
         dwq = dwk = ws = None
@@ -328,7 +325,7 @@ class Mixers:
         _i32(ints[0], ints[1], B)
         _f32("lse", lse, (B, Hq, T))
         st = [(_I64 * 3)() if n not in ts else (_strides3 if ts[n].dim() == 4 else _strides_decode)(ts[n]) for n in self._ORDER]
-        return _new(key, WindowParams(B, T, Hq, Hk, d, _dtype_code(first), window, sinks, 0.0, 0, *st))
+        return self._new(key, WindowParams(B, T, Hq, Hk, d, _dtype_code(first), window, sinks, 0.0, 0, *st))
 
     def lasad_window_attention(self, q, k, v, window, sinks=0, scale=None, lengths=None, o=None, lse=None,
                                want_lse=False, stream=None):
@@ -338,8 +335,8 @@ class Mixers:
         gradient needs it)."""
         if o is None:
             o = _like(q)
-        key = ("window", self.device, window, sinks, _look(q), _look(k), _look(v), _look(lengths), _look(o), _look(lse))
-        e = _cache.get(key) or self._window(key, "forward", window, sinks, lse, ("lengths", lengths), q=q, k=k, v=v, o=o)
+        key = ("window", window, sinks, _look(q), _look(k), _look(v), _look(lengths), _look(o), _look(lse))
+        e = self._calls.get(key) or self._window(key, "forward", window, sinks, lse, ("lengths", lengths), q=q, k=k, v=v, o=o)
         p = e.p
         p.scale = 1.0 / math.sqrt(p.d) if scale is None else scale
         if lse is None and want_lse:
@@ -356,9 +353,9 @@ class Mixers:
         dq = _like(q) if dq is None else dq
         dk = _like(k) if dk is None else dk
         dv = _like(v) if dv is None else dv
-        key = ("window'", self.device, window, sinks, _look(q), _look(k), _look(v), _look(o), _look(lse), _look(do),
+        key = ("window'", window, sinks, _look(q), _look(k), _look(v), _look(o), _look(lse), _look(do),
                _look(lengths), _look(dq), _look(dk), _look(dv))
-        e = _cache.get(key)
+        e = self._calls.get(key)
         if e is None:
             if lse is None:
                 raise ValueError("lse is what lasad_window_attention returns with want_lse=True")
@@ -381,9 +378,9 @@ class Mixers:
         (negative: the sequence takes no part).  Returns o [B,Hq,d]."""
         if o is None:
             o = _like(q)
-        key = ("window1", self.device, window, sinks, _look(q), _look(k), _look(v), _look(k_cache), _look(v_cache), _look(pos),
+        key = ("window1", window, sinks, _look(q), _look(k), _look(v), _look(k_cache), _look(v_cache), _look(pos),
                _look(o))
-        e = _cache.get(key)
+        e = self._calls.get(key)
         if e is None:
             if pos is None:
                 raise ValueError("pos must be contiguous int32 [B]")
@@ -399,8 +396,8 @@ class Mixers:
 
     def lasad_window_cache_store(self, k, v, k_cache, v_cache, window, sinks=0, lengths=None, stream=None):
         """Puts the keys and values of a prefill, [B,T,Hk,d], into the ring caches of the step."""
-        key = ("store", self.device, window, sinks, _look(k), _look(v), _look(k_cache), _look(v_cache), _look(lengths))
-        e = _cache.get(key) or self._window(key, "store", window, sinks, None, ("lengths", lengths), k=k, v=v, k_cache=k_cache,
+        key = ("store", window, sinks, _look(k), _look(v), _look(k_cache), _look(v_cache), _look(lengths))
+        e = self._calls.get(key) or self._window(key, "store", window, sinks, None, ("lengths", lengths), k=k, v=v, k_cache=k_cache,
                                             v_cache=v_cache)
         rc = self._lib.lasad_window_cache_store(self._h, e.ref, k.data_ptr(), v.data_ptr(), _ptr(lengths), k_cache.data_ptr(),
                                                 v_cache.data_ptr(), _stream(k.device, stream))

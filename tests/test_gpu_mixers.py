@@ -377,6 +377,40 @@ def test_window_long_ragged_against_the_other_implementation_and_repeats(ctx, dt
         assert torch.equal(a, b) and torch.equal(a[1:2], c)
 
 
+def test_window_back_to_back_in_a_warm_cache(ctx):
+    """A long case over and over: tiles land at once, so that every wait meets the barrier's phase that
+    is the hardest to tell from the next; no wait may give up, and every launch returns the same bits."""
+    _, (q, k, v, do) = window_case(1, 2305, 8, 4, 64, BF16, None, 6)
+    first = None
+    for _ in range(30):
+        o, lse = ctx.lasad_window_attention(q, k, v, 700, 3, want_lse=True)
+        got = (o, lse) + ctx.lasad_window_attention_backward(q, k, v, o, lse, do, 700, 3)
+        first = first or got
+    torch.cuda.synchronize()
+    assert ctx.device_status() == 0
+    assert all(torch.equal(a, b) for a, b in zip(first, got))
+
+
+def test_window_waits_are_bounded(ctx):
+    """Waits that run out after one try: the kernels report it and leave, and the next calls are whole."""
+    _, (q, k, v, do) = window_case(1, 700, 4, 4, 64, BF16, None, 7)
+    o, lse = ctx.lasad_window_attention(q, k, v, 300, 1, want_lse=True)
+    want = ctx.lasad_window_attention_backward(q, k, v, o, lse, do, 300, 1)
+    try:
+        ctx.set_option(binding.LASAD_OPT_WAIT_LIMIT, 1)
+        ctx.lasad_window_attention(q, k, v, 300, 1)
+        torch.cuda.synchronize()
+        assert ctx.device_status() == binding.LASAD_ERR_TIMEOUT
+        ctx.lasad_window_attention_backward(q, k, v, o, lse, do, 300, 1)
+        torch.cuda.synchronize()
+        assert ctx.device_status() == binding.LASAD_ERR_TIMEOUT
+    finally:
+        ctx.set_option(binding.LASAD_OPT_WAIT_LIMIT, 0)
+    assert torch.equal(ctx.lasad_window_attention(q, k, v, 300, 1)[0], o)
+    assert all(torch.equal(a, b) for a, b in zip(ctx.lasad_window_attention_backward(q, k, v, o, lse, do, 300, 1), want))
+    assert ctx.device_status() == 0
+
+
 STEP = [  # B, Hq, Hk, d, window, sinks
     (1, 1, 1, 64, 1, 0), (3, 2, 1, 64, 5, 0), (4, 3, 3, 32, 16, 2), (2, 8, 1, 64, 200, 1), (5, 12, 4, 64, 64, 1),
     (2, 10, 1, 64, 33, 3), (1, 24, 8, 64, 1500, 1), (40, 4, 4, 64, 70, 4),
@@ -485,6 +519,15 @@ def test_raw_stream_handle_keeps_its_workspace(ctx):
         torch.empty(1 << 16, device="cuda").fill_(float("nan"))
     torch.cuda.synchronize()
     assert all(torch.equal(o, want) for o in outs)
+
+
+def test_hybrid_block_example():
+    """The operators together: a training step lowers the loss, and a prefix continued token by token
+    gives the rows of one pass (bf16 projections of bf16 sums on both sides: a few roundings)."""
+    from examples import hybrid_block
+    losses = hybrid_block.train(steps=10)
+    assert losses[-1] < 0.9 * losses[0]
+    assert hybrid_block.generate(T=120) < 2e-2
 
 
 def test_launches_are_counted(ctx):

@@ -148,17 +148,25 @@ __device__ __forceinline__ bool window_sees(int t, int s, int window, int sinks,
 }
 #endif
 
-// Delta of every row, and the gradients of the sinks' keys and values from the queries whose window
-// has left them, in sums over kPrepRows rows (see lasad_window_prep.cu).
+// The backward's workspace: what it needs of each row, and the gradients of the sinks' keys and values
+// from the queries whose window has left them, in sums over kPrepRows rows (see lasad_window_prep.cu).
+// Of kPrepRows rows of a query head at a time first -lse log2(e), then -Delta (a block is 512 bytes
+// on a 16-byte boundary, which a bulk copy can take); behind them the sums [B,Hk,ceil(T/kPrepRows),sinks,2,d].
 constexpr int kPrepRows = 64;
-// floats of the backward's workspace: Delta [B,Hq,T], then the sinks' sums [B,Hk,ceil(T/kPrepRows),sinks,2,d]
-__host__ __device__ inline size_t window_delta_floats(const WindowArgs& a) { return ((size_t)a.B * a.Hq * a.T + 3) / 4 * 4; }
+__host__ __device__ inline long long window_stat_at(int T, long long bh, int t)
+{
+    return (bh * ((T + kPrepRows - 1) / kPrepRows) + t / kPrepRows) * (2 * kPrepRows) + t % kPrepRows;
+}
+__host__ __device__ inline size_t window_stat_floats(const WindowArgs& a) { return (size_t)window_stat_at(a.T, (long long)a.B * a.Hq, 0); }
 size_t window_workspace_bytes(const WindowArgs& a);
-cudaError_t launch_window_prep(const WindowArgs& a, cudaStream_t st);
+// Fills the workspace (delta), or the sums alone from what stands there of the rows.
+cudaError_t launch_window_prep(const WindowArgs& a, bool delta, cudaStream_t st);
 cudaError_t launch_window_forward_tc(const WindowArgs& a, cudaStream_t st);      // bf16
-cudaError_t launch_window_backward_tc(const WindowArgs& a, cudaStream_t st);     // two launches, behind launch_window_prep
+// (two launches, with launch_window_prep between them where a window leaves a sink)
+cudaError_t launch_window_backward_tc(const WindowArgs& a, cudaStream_t st);
+inline int window_backward_tc_launches(const WindowArgs& a) { return a.sinks > 0 && a.window < a.T ? 3 : 2; }
 cudaError_t launch_window_forward_simt(const WindowArgs& a, cudaStream_t st);
-cudaError_t launch_window_backward_simt(const WindowArgs& a, cudaStream_t st);   // two launches, behind launch_window_prep
+cudaError_t launch_window_backward_simt(const WindowArgs& a, cudaStream_t st);   // three launches
 // One token against the ring cache.
 cudaError_t launch_window_step(const WindowArgs& a, cudaStream_t st);
 cudaError_t launch_window_store(const WindowArgs& a, cudaStream_t st);

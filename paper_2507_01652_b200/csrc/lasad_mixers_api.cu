@@ -304,9 +304,8 @@ int lasad_window_attention_backward(lasad_ctx* ctx, const lasad_window_params* p
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const int impl = window_impl(ctx, a);
     if (impl < 0) return impl;
-    cudaError_t e = lasad::launch_window_prep(a, st);
-    if (e == cudaSuccess) e = impl == 2 ? lasad::launch_window_backward_tc(a, st) : lasad::launch_window_backward_simt(a, st);
-    return launched(ctx, e, 3);
+    return impl == 2 ? launched(ctx, lasad::launch_window_backward_tc(a, st), lasad::window_backward_tc_launches(a))
+                     : launched(ctx, lasad::launch_window_backward_simt(a, st), 3);
 }
 
 int lasad_window_attention_step(lasad_ctx* ctx, const lasad_window_params* p, const void* q, const void* k,

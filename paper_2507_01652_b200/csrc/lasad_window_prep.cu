@@ -1,6 +1,6 @@
-// What the gradient of the window attention needs before its products:
+// What the gradient of the window attention needs beside its products:
 //
-//     Delta_t = sum_c do_tc o_tc        (per query head),
+//     Delta_t = sum_c do_tc o_tc        (per query head; the tensor-core kernels form it themselves),
 //
 // and, for the sinks (tokens s < S, visible to every later query), the gradients from the queries
 // that see s only because it is a sink, t >= s + W:
@@ -36,7 +36,7 @@ __device__ __forceinline__ void load_piece(const T* p, float (&v)[N])
 
 constexpr int kWarps = 8, kAhead = 3;
 
-template <typename T, int D>
+template <typename T, int D, bool DELTA>
 __global__ void __launch_bounds__(32 * kWarps) window_prep_kernel(const WindowArgs a)
 {
     constexpr int N = sizeof(T) == 2 ? 8 : 4, LANES = D / N, ROWS = 32 / LANES;
@@ -51,7 +51,7 @@ __global__ void __launch_bounds__(32 * kWarps) window_prep_kernel(const WindowAr
     const T* g = static_cast<const T*>(a.dout) + b * a.dos[0] + sub * N;
     const T* q = static_cast<const T*>(a.q) + b * a.qs[0] + sub * N;
     // (kAhead rows of each lane group at a time: their loads are in flight together)
-    for (int r0 = 0; r0 < rows * G; r0 += kWarps * ROWS * kAhead) {
+    for (int r0 = 0; DELTA && r0 < rows * G; r0 += kWarps * ROWS * kAhead) {
         float ov[kAhead][N], gv[kAhead][N];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
@@ -68,14 +68,14 @@ __global__ void __launch_bounds__(32 * kWarps) window_prep_kernel(const WindowAr
 #pragma unroll
             for (int k = LANES / 2; k >= 1; k >>= 1) d += __shfl_xor_sync(0xffffffffu, d, k);
             // (a row past its sequence's end counts for nothing, whatever stands in o and do)
-            if (r < rows * G && sub == 0) a.ws[((long long)b * a.Hq + h) * a.T + t] = t < len ? d : 0.0f;
+            if (r < rows * G && sub == 0)
+                a.ws[window_stat_at(a.T, (long long)b * a.Hq + h, t) + kPrepRows] = t < len ? -d : 0.0f;
         }
     }
     const int sinks = min(a.sinks, a.T);
     if (sinks == 0 || t0 + rows <= a.window || t0 >= len) return;   // (uniform over the CTA)
-    __syncthreads();                                                // Delta of the CTA's rows
-    const float* delta = a.ws;
-    float* sums = a.ws + window_delta_floats(a) + ((long long)bh * chunks + chunk) * sinks * 2 * D;
+    if (DELTA) __syncthreads();                                     // what the CTA's rows have left
+    float* sums = a.ws + window_stat_floats(a) + ((long long)bh * chunks + chunk) * sinks * 2 * D;
     constexpr float kLog2e = 1.4426950408889634f;
     for (int s = 0; s < sinks; ++s) {
         float kv[N], vv[N], dk[N], dv[N];
@@ -90,11 +90,11 @@ __global__ void __launch_bounds__(32 * kWarps) window_prep_kernel(const WindowAr
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
                 const int r = min(r0 + (i * kWarps + warp) * ROWS + mine, n - 1), t = t0 + lo + r / G, h = hk * G + r % G;
-                const long long at = ((long long)b * a.Hq + h) * a.T + t;
                 load_piece<T, N>(q + t * a.qs[1] + h * a.qs[2], qv[i]);
                 load_piece<T, N>(g + t * a.dos[1] + h * a.dos[2], gv[i]);
-                ls[i] = a.lse[at];
-                de[i] = delta[at];
+                const long long bhq = (long long)b * a.Hq + h;
+                ls[i] = a.lse[bhq * a.T + t];
+                de[i] = a.ws[window_stat_at(a.T, bhq, t) + kPrepRows];      // -Delta
             }
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(32 * kWarps) window_prep_kernel(const WindowAr
                     y += __shfl_xor_sync(0xffffffffu, y, k);
                 }
                 if (r0 + (i * kWarps + warp) * ROWS + mine < n) {
-                    const float p = exp2f((x * a.scale - ls[i]) * kLog2e), ds = p * (y - de[i]) * a.scale;
+                    const float p = exp2f((x * a.scale - ls[i]) * kLog2e), ds = p * (y + de[i]) * a.scale;
 #pragma unroll
                     for (int e = 0; e < N; ++e) dk[e] = fmaf(ds, qv[i][e], dk[e]), dv[e] = fmaf(p, gv[i][e], dv[e]);
                 }
@@ -133,20 +133,25 @@ __global__ void __launch_bounds__(32 * kWarps) window_prep_kernel(const WindowAr
     }
 }
 
+template <bool DELTA> cudaError_t launch_prep(const WindowArgs& a, cudaStream_t st)
+{
+    const unsigned n = (unsigned)((a.T + kPrepRows - 1) / kPrepRows) * a.B * a.Hk;
+    auto kernel = a.bf16 ? (a.d == 64 ? window_prep_kernel<__nv_bfloat16, 64, DELTA> : window_prep_kernel<__nv_bfloat16, 32, DELTA>)
+                         : (a.d == 64 ? window_prep_kernel<float, 64, DELTA> : window_prep_kernel<float, 32, DELTA>);
+    return launch_dependent(kernel, dim3(n), dim3(32 * kWarps), 0, st, a);
+}
+
 }  // namespace
 
 size_t window_workspace_bytes(const WindowArgs& a)
 {
     const size_t chunks = (a.T + kPrepRows - 1) / kPrepRows, sinks = a.sinks < a.T ? a.sinks : a.T;
-    return (window_delta_floats(a) + (size_t)a.B * a.Hk * chunks * sinks * 2 * a.d) * sizeof(float);
+    return (window_stat_floats(a) + (size_t)a.B * a.Hk * chunks * sinks * 2 * a.d) * sizeof(float);
 }
 
-cudaError_t launch_window_prep(const WindowArgs& a, cudaStream_t st)
+cudaError_t launch_window_prep(const WindowArgs& a, bool delta, cudaStream_t st)
 {
-    const unsigned n = (unsigned)((a.T + kPrepRows - 1) / kPrepRows) * a.B * a.Hk;
-    auto kernel = a.bf16 ? (a.d == 64 ? window_prep_kernel<__nv_bfloat16, 64> : window_prep_kernel<__nv_bfloat16, 32>)
-                         : (a.d == 64 ? window_prep_kernel<float, 64> : window_prep_kernel<float, 32>);
-    return launch_dependent(kernel, dim3(n), dim3(32 * kWarps), 0, st, a);
+    return delta ? launch_prep<true>(a, st) : launch_prep<false>(a, st);
 }
 
 }  // namespace lasad

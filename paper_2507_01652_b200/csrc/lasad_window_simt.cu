@@ -233,7 +233,7 @@ __device__ __forceinline__ void gradient_scores(SmemBwd<D>& sm, const WindowArgs
             const bool sees = window_sees(t, k0 + col, a.window, all ? a.sinks : 0, len);
             const float p = sees ? exp2f((s[i][c] * a.scale - sm.lse[ty * 4 + i]) * kLog2e) : 0.0f;
             sm.p.x[ty * 4 + i][col] = p;
-            sm.s.x[ty * 4 + i][col] = sees ? p * (d[i][c] - sm.delta[ty * 4 + i]) * a.scale : 0.0f;
+            sm.s.x[ty * 4 + i][col] = sees ? p * (d[i][c] + sm.delta[ty * 4 + i]) * a.scale : 0.0f;
         }
     }
 }
@@ -246,7 +246,7 @@ __device__ __forceinline__ void load_queries(SmemBwd<D>& sm, const WindowArgs& a
         const int t = q0 + threadIdx.x;
         const long long at = ((long long)b * a.Hq + h) * a.T + t;
         sm.lse[threadIdx.x] = t < len ? a.lse[at] : 0.0f;
-        sm.delta[threadIdx.x] = t < len ? a.ws[at] : 0.0f;
+        sm.delta[threadIdx.x] = t < len ? a.ws[window_stat_at(a.T, (long long)b * a.Hq + h, t) + kPrepRows] : 0.0f;   // -Delta
     }
 }
 
@@ -286,7 +286,7 @@ __global__ void __launch_bounds__(kThreads) window_dkdv_simt_kernel(const Window
         const int s = k0 + ty * 4 + i;
         if (s >= a.T) continue;
         if (s < sinks && a.window < len) {      // the sums of launch_window_prep: chunks with a row past the window, before the end
-            const float* sums = a.ws + window_delta_floats(a) + ((long long)bh * chunks * sinks + s) * 2 * D;
+            const float* sums = a.ws + window_stat_floats(a) + ((long long)bh * chunks * sinks + s) * 2 * D;
             for (int c = a.window / kPrepRows; c < (len + kPrepRows - 1) / kPrepRows; ++c) {
                 const float* w = sums + (long long)c * sinks * 2 * D;
 #pragma unroll
@@ -366,6 +366,8 @@ cudaError_t launch_window_forward_simt(const WindowArgs& a, cudaStream_t st)
 }
 cudaError_t launch_window_backward_simt(const WindowArgs& a, cudaStream_t st)
 {
+    const cudaError_t e = launch_window_prep(a, true, st);
+    if (e != cudaSuccess) return e;
     if (a.bf16) return a.d == 64 ? backward_t<__nv_bfloat16, 64>(a, st) : backward_t<__nv_bfloat16, 32>(a, st);
     return a.d == 64 ? backward_t<float, 64>(a, st) : backward_t<float, 32>(a, st);
 }

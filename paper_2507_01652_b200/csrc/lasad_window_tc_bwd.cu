@@ -8,13 +8,21 @@
 // tile of 64 rows that it passes (Q, dO or K, V), a tile costs the products
 //
 //     S = X1 Y1^T ,  dP = X2 Y2^T ,        P = 2^(S c - lse log2(e)) ,  dS = P * (dP - Delta)
-//     A1 += dS Y1  (dK or dQ) ,            keys only: A2 += P Y2  (dV)
+//     A1 += dS Y1  (dK or dQ) ,            A2 += P Y2 (dV)  or  P Y1
 //
 // all of them tcgen05 128 x 64 x 64 with the left operand in TMEM: X1 and X2 are put there once, and P
 // and dS are written over S and dP.  (A left operand from shared memory would cost 4 KB beside the 2 KB
 // of the right one per 32-clock instruction, more than the 128 bytes per clock that an SM reads.)
-// scale is applied to dK and dQ once, at the end.  Delta and, for the keys of the sinks, the sums
-// over the queries whose window has left them come from launch_window_prep.
+// scale is applied to dK and dQ once, at the end.
+//
+// Delta.  The queries kernel runs first and starts from Delta' = sum_c do_c o_c, but the o that a caller
+// has was rounded to bf16, and where a row sees few keys, dP - Delta is small against what that
+// rounding does to Delta' (two keys: 0.6 % of dQ, three times what bf16 itself costs).  So it sums
+// r = sum_s P (dP - Delta') in fp32 beside its products -- Delta = Delta' + r, as the P of a row add up to 1 --
+// and ends with dQ = A1 - r A2, A2 = P K.  It leaves -lse log2(e) and -Delta to the keys kernel (and to the
+// sums over the queries whose window has left the sinks, launch_window_prep, which runs between the
+// two), in blocks of 64 rows that come with the tiles.  P and dS enter their products in bf16, as the
+// tensor cores take them: 2^-9 of each term, which adds up like noise.
 //
 // What bounds it: per tile 512 clocks of exponentials (16 per SM and clock) against four (three)
 // products of 128 clocks.  Two groups of eight warps take the tiles in turn, each with its own S
@@ -33,21 +41,25 @@ namespace {
 
 using namespace tcx;
 
-constexpr int kRows = 128, kCols = 64, kStages = 4, kGroup = 256, kThreads = 2 * kGroup + 64;
+constexpr int kRows = 128, kCols = 64, kStages = 4, kGroup = 256, kThreads = 2 * kGroup + 96;
 constexpr int kTile = kCols * 128;                         // bytes of a passing tile
 constexpr uint32_t kColX1 = 0, kColX2 = 32, kColS = 64, kColDP = 128, kGroupCols = 128, kColA1 = 320, kColA2 = 384;
+constexpr uint32_t kColP = 448, kColDS = 480;
 constexpr int kTmemCols = 512;
 
 struct Smem {
     unsigned char y1[kStages][kTile];
     unsigned char y2[kStages][kTile];
-    float lse[2][2][kCols], delta[2][2][kCols];            // keys: of each group's tiles, by column, two in turn
+    float stat[kStages][2][kCols];                         // keys: -lse log2(e) and -Delta of the tile's rows
+    float part[2][kRows], rest[4][kRows];                  // queries: halves of Delta', quarters of r
     unsigned long long full[kStages], free[kStages];       // Y1 and Y2 have landed; their products have been made
-    unsigned long long x_ready;                            // X1 and X2 are in TMEM (2 kGroup arrivals)
-    unsigned long long s_full[2];                          // S and dP of a group's tile are there (and all products before are done)
-    unsigned long long p_ready[2];                         // P and dS are (kGroup arrivals)
-    unsigned long long st_ready[2];                        // keys: lse and delta are (kGroup arrivals)
-    unsigned long long done, drain;
+    unsigned long long x_ready;                            // X1 and X2 are in TMEM, queries: Delta' is in part (2 kGroup arrivals)
+    unsigned long long s_full[2];                          // S and dP of a group's tile are there
+    unsigned long long s_free[2];                          // ... and have been read (kGroup arrivals)
+    unsigned long long p_ready[2];                         // P and dS of a group's tile are there (kGroup arrivals)
+    unsigned long long p_free[2];                          // ... and their products have been made
+    unsigned long long r_ready;                            // queries: r is in rest (2 kGroup arrivals)
+    unsigned long long done, drain[2];
     uint32_t tmem_base;
     int abort_flag;
 };
@@ -56,12 +68,13 @@ struct Params {
     int B, T, Hq, Hk, d, window, sinks;
     float scale, scale2;                                   // scale2 = scale log2(e)
     const int* lengths;
-    const float* lse;
-    const float* delta;
+    const float* lse;                                      // queries: [B,Hq,T]
+    float* stat;                                           // see window_stat_at
     const float* sums;                                     // keys: of the sinks, [B,Hk,chunks,sinks,2,d]
     const __nv_bfloat16* x1;
     const __nv_bfloat16* x2;
-    long long x1s[3], x2s[3];
+    const __nv_bfloat16* o;                                // queries
+    long long x1s[3], x2s[3], os[3];
     __nv_bfloat16* a1;
     __nv_bfloat16* a2;
     long long a1s[3], a2s[3];
@@ -69,17 +82,15 @@ struct Params {
     unsigned wait_limit;
 };
 
-// 32 channels of a row of an own operand into 16 TMEM columns.
-__device__ __forceinline__ void half_row_to_tmem(uint32_t col, const __nv_bfloat16* row, bool live)
+// 32 channels of a row, or zeros.
+__device__ __forceinline__ void half_row(const __nv_bfloat16* row, bool live, uint32_t (&r)[16])
 {
-    uint32_t r[16];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         uint4 v = make_uint4(0, 0, 0, 0);
         if (live) v = *reinterpret_cast<const uint4*>(row + 8 * i);
         r[4 * i] = v.x, r[4 * i + 1] = v.y, r[4 * i + 2] = v.z, r[4 * i + 3] = v.w;
     }
-    tmem_st16(col, r);
 }
 
 template <bool KEYS>
@@ -105,11 +116,13 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
         mbar_init(&sm.x_ready, 2 * kGroup);
         for (int w = 0; w < 2; ++w) {
             mbar_init(&sm.s_full[w], 1);
+            mbar_init(&sm.s_free[w], kGroup);
             mbar_init(&sm.p_ready[w], kGroup);
-            mbar_init(&sm.st_ready[w], kGroup);
+            mbar_init(&sm.p_free[w], 1);
+            mbar_init(&sm.drain[w], 1);
         }
+        mbar_init(&sm.r_ready, 2 * kGroup);
         mbar_init(&sm.done, 1);
-        mbar_init(&sm.drain, 1);
         sm.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -152,9 +165,12 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
             for (; issued < n; ++issued) {
                 const int s = issued % kStages;
                 if (issued >= kStages && !mbar_wait(&sm.free[s], (issued / kStages - 1) & 1, limit, abort_flag, p.status)) break;
-                mbar_arrive_expect_tx(&sm.full[s], 2 * kTile);
+                mbar_arrive_expect_tx(&sm.full[s], 2 * kTile + (KEYS ? 8 * kCols : 0));
                 tma_load_4d(sm.y1[s], &tm_y1, &sm.full[s], 0, head_of(issued), first_of(issued), b);
                 tma_load_4d(sm.y2[s], &tm_y2, &sm.full[s], 0, head_of(issued), first_of(issued), b);
+                if (KEYS)
+                    bulk_load(sm.stat[s], p.stat + window_stat_at(p.T, (long long)b * p.Hq + head_of(issued), first_of(issued)),
+                              8 * kCols, &sm.full[s]);
             }
             // leave only when every issued load has landed
             for (int j = max(0, issued - kStages); j < issued; ++j)
@@ -162,61 +178,63 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
                     if (mbar_try_wait(&sm.full[j % kStages], (j / kStages) & 1)) break;
         }
         __syncwarp();
-    } else if (warp == 16) {
+    } else if (warp == 18) {
+        // ===================== S and dP of every tile =====================
         const uint64_t dy1 = make_desc(smem_u32(sm.y1[0])), dy2 = make_desc(smem_u32(sm.y2[0]));
         constexpr uint64_t stage = kTile >> 4;
-        constexpr uint32_t idesc_s = make_idesc(128, 64, 0, 0);    // X (tmem) x Y (K-major)
-        constexpr uint32_t idesc_a = make_idesc(128, 64, 0, 1);    // P, dS (tmem) x Y (MN-major)
-        // (the elected lane) S and dP of tile i
-        auto scores = [&](int i) {
-            const int s = i % kStages, w = i & 1;
-            const uint32_t at_s = tmem + kColS + w * kGroupCols, at_dp = tmem + kColDP + w * kGroupCols;
-#pragma unroll
-            for (int kk = 0; kk < 4; ++kk) mma_ts(at_s, tmem + kColX1 + 8 * kk, dy1 + s * stage + 2 * kk, idesc_s, kk > 0);
-#pragma unroll
-            for (int kk = 0; kk < 4; ++kk) mma_ts(at_dp, tmem + kColX2 + 8 * kk, dy2 + s * stage + 2 * kk, idesc_s, kk > 0);
-        };
-        auto landed = [&](int i) { return warp_wait(&sm.full[i % kStages], (i / kStages) & 1, limit, abort_flag, p.status); };
+        constexpr uint32_t idesc = make_idesc(128, 64, 0, 0);      // X (tmem) x Y (K-major)
         bool ok = n > 0 && warp_wait(&sm.x_ready, 0, limit, abort_flag, p.status);
-        for (int i = 0; ok && i < min(n, 2); ++i) {
-            if (!(ok = landed(i))) break;
+        for (int i = 0; ok && i < n; ++i) {
+            const int s = i % kStages, w = i & 1;
+            if (i >= 2 && !(ok = warp_wait(&sm.s_free[w], ((i >> 1) - 1) & 1, limit, abort_flag, p.status))) break;
+            if (!(ok = warp_wait(&sm.full[s], (i / kStages) & 1, limit, abort_flag, p.status))) break;
             tc_fence_after();
             if (elect_one()) {
-                scores(i);
-                mma_commit(&sm.s_full[i]);
+                const uint32_t at_s = tmem + kColS + w * kGroupCols, at_dp = tmem + kColDP + w * kGroupCols;
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk) mma_ts(at_s, tmem + kColX1 + 8 * kk, dy1 + s * stage + 2 * kk, idesc, kk > 0);
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk) mma_ts(at_dp, tmem + kColX2 + 8 * kk, dy2 + s * stage + 2 * kk, idesc, kk > 0);
+                mma_commit(&sm.s_full[w]);
             }
             __syncwarp();
         }
+        // (no product may still run when the CTA's memory goes)
+        if (elect_one()) {
+            mma_commit(&sm.drain[0]);
+            for (unsigned it = 0; it < kDrainLimit; ++it)
+                if (mbar_try_wait(&sm.drain[0], 0)) break;
+        }
+        __syncwarp();
+    } else if (warp == 16) {
+        // ===================== what P and dS add to A2 and A1, tile after tile =====================
+        const uint64_t dy1 = make_desc(smem_u32(sm.y1[0])), dy2 = make_desc(smem_u32(sm.y2[0]));
+        constexpr uint64_t stage = kTile >> 4;
+        constexpr uint32_t idesc = make_idesc(128, 64, 0, 1);      // P, dS (tmem) x Y (MN-major)
+        bool ok = true;
         for (int i = 0; ok && i < n; ++i) {
             const int s = i % kStages, w = i & 1;
-            // (the wait for a tile that has most often landed long ago stands ahead of the one for P)
-            if (i + 2 < n && !(ok = landed(i + 2))) break;
+            if (!(ok = warp_wait(&sm.full[s], (i / kStages) & 1, limit, abort_flag, p.status))) break;
             if (!(ok = warp_wait(&sm.p_ready[w], (i >> 1) & 1, limit, abort_flag, p.status))) break;
             tc_fence_after();
             if (elect_one()) {
-                const uint32_t at_p = tmem + kColS + w * kGroupCols, at_ds = tmem + kColDP + w * kGroupCols;
-                // 16 passing rows: 8 columns of P or dS (rows 32-63 stand 32 columns on), 2048 bytes of Y
-                if (KEYS)
-#pragma unroll
-                    for (int kk = 0; kk < 4; ++kk)
-                        mma_ts(tmem + kColA2, at_p + 32 * (kk >> 1) + 8 * (kk & 1), dy2 + s * stage + 128 * kk, idesc_a, i > 0 || kk > 0);
+                // 16 passing rows: 8 columns of P or dS, 2048 bytes of Y
 #pragma unroll
                 for (int kk = 0; kk < 4; ++kk)
-                    mma_ts(tmem + kColA1, at_ds + 32 * (kk >> 1) + 8 * (kk & 1), dy1 + s * stage + 128 * kk, idesc_a, i > 0 || kk > 0);
+                    mma_ts(tmem + kColA2, tmem + kColP + 8 * kk, (KEYS ? dy2 : dy1) + s * stage + 128 * kk, idesc, i > 0 || kk > 0);
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk)
+                    mma_ts(tmem + kColA1, tmem + kColDS + 8 * kk, dy1 + s * stage + 128 * kk, idesc, i > 0 || kk > 0);
+                mma_commit(&sm.p_free[w]);
                 mma_commit(&sm.free[s]);
-                // the group's next S and dP, over this P and dS (the products run in the order they were issued)
-                if (i + 2 < n) {
-                    scores(i + 2);
-                    mma_commit(&sm.s_full[w]);
-                }
                 if (i == n - 1) mma_commit(&sm.done);
             }
             __syncwarp();
         }
         if (elect_one()) {
-            mma_commit(&sm.drain);
+            mma_commit(&sm.drain[1]);
             for (unsigned it = 0; it < kDrainLimit; ++it)
-                if (mbar_try_wait(&sm.drain, 0)) break;
+                if (mbar_try_wait(&sm.drain[1], 0)) break;
         }
         __syncwarp();
     } else {
@@ -225,41 +243,39 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const int rw0 = r0 + (warp & 3) * 32, rw1 = rw0 + 31;     // the warp's rows
         // X1 by group 0, X2 by group 1, half a row each
+        const bool mine = r < len && 32 * c < p.d;
         {
             const __nv_bfloat16* x = group == 0 ? p.x1 + b * p.x1s[0] + r * p.x1s[1] + h * p.x1s[2]
                                                 : p.x2 + b * p.x2s[0] + r * p.x2s[1] + h * p.x2s[2];
-            half_row_to_tmem(lanes + (group == 0 ? kColX1 : kColX2) + 16 * c, x + 32 * c, r < len && 32 * c < p.d);
+            uint32_t xv[16];
+            half_row(x + 32 * c, mine, xv);
+            tmem_st16(lanes + (group == 0 ? kColX1 : kColX2) + 16 * c, xv);
+            if (!KEYS && group == 1) {
+                uint32_t ov[16];
+                half_row(p.o + b * p.os[0] + r * p.os[1] + h * p.os[2] + 32 * c, mine, ov);
+                float sum = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sum = fmaf(bf16_lo(xv[e]), bf16_lo(ov[e]), fmaf(bf16_hi(xv[e]), bf16_hi(ov[e]), sum));
+                sm.part[c][row] = sum;
+            }
         }
         tmem_wait_st();
         tc_fence_before();
         mbar_arrive(&sm.x_ready);
 
-        float row_lse = 0.0f, row_delta = 0.0f;
-        if (!KEYS && r < len) {
-            row_lse = -p.lse[(long long)bh * p.T + r] * kLog2e;
-            row_delta = -p.delta[(long long)bh * p.T + r];
-        }
-        // keys: this thread's part of the tile's 64 lse (threads 0-63) and Delta (64-127; the rest has none), one tile ahead
-        auto stat = [&](int i) {
-            const int q = first_of(i) + (gt & 63);
-            if (gt >= 128 || q >= len) return 0.0f;
-            const long long x = ((long long)b * p.Hq + head_of(i)) * p.T + q;
-            return gt < 64 ? -p.lse[x] * kLog2e : -p.delta[x];
-        };
-        float ahead = KEYS && group < n ? stat(group) : 0.0f;
         bool ok = true;
-        for (int i = group; i < n; i += 2) {
+        float row_lse = 0.0f, row_delta = 0.0f, rest[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (!KEYS && n > 0 && (ok = warp_wait(&sm.x_ready, 0, limit, abort_flag, p.status)) && r < len) {
+            row_lse = -p.lse[(long long)bh * p.T + r] * kLog2e;
+            row_delta = -(sm.part[0][row] + sm.part[1][row]);
+        }
+        for (int i = group; ok && i < n; i += 2) {
             const int s = i % kStages, c0 = first_of(i);
-            if (KEYS) {
-                // (a buffer is written again two tiles on, when every thread has arrived for the one between)
-                if (gt < 128) (gt < 64 ? sm.lse : sm.delta)[group][(i >> 1) & 1][gt & 63] = ahead;
-                mbar_arrive(&sm.st_ready[group]);
-                if (i + 2 < n) ahead = stat(i + 2);
-                if (!(ok = warp_wait(&sm.st_ready[group], (i >> 1) & 1, limit, abort_flag, p.status))) break;
-            }
+            // (the tile's statistics; a group has every other tile, so it sees every phase of its places, and a
+            // place's next phase needs this tile's products)
+            if (KEYS && !(ok = warp_wait(&sm.full[s], (i / kStages) & 1, limit, abort_flag, p.status))) break;
             if (!(ok = warp_wait(&sm.s_full[group], (i >> 1) & 1, limit, abort_flag, p.status))) break;
             tc_fence_after();
-            const uint32_t at_s = lanes + kColS + group * kGroupCols, at_dp = lanes + kColDP + group * kGroupCols;
             {
                 // what the warp's rows and these 32 columns have to do with each other: 0 nothing, 1 part, 2 all
                 const int s0 = c0 + 32 * c, s1 = s0 + 31;
@@ -274,42 +290,60 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
                 uint32_t pp[16], pd[16];
                 if (any) {
                     uint32_t sv[32], dv[32];
-                    tmem_ld32(at_s + 32 * c, sv);
-                    tmem_ld32(at_dp + 32 * c, dv);
+                    tmem_ld32(lanes + kColS + group * kGroupCols + 32 * c, sv);
+                    tmem_ld32(lanes + kColDP + group * kGroupCols + 32 * c, dv);
                     tmem_wait_ld();
+                    tc_fence_before();
+                    mbar_arrive(&sm.s_free[group]);
+                    // (what is masked may be NaN: its bits go)
+                    uint32_t bits = 0xffffffffu;
+                    if (!all)
+                        bits = r >= len ? 0u : KEYS ? bit_range(r - s0, min(r + p.window - 1, len - 1) - s0)
+                                                    : seen_bits(r, s0, p.window, p.sinks, len);
+                    float4 ls = make_float4(row_lse, row_lse, row_lse, row_lse), de = make_float4(row_delta, row_delta, row_delta, row_delta);
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         float x0, x1, g0 = __uint_as_float(dv[2 * e]), g1 = __uint_as_float(dv[2 * e + 1]);
-                        float2 ls = make_float2(row_lse, row_lse), de = make_float2(row_delta, row_delta);
-                        if (KEYS) {
-                            ls = *reinterpret_cast<const float2*>(&sm.lse[group][(i >> 1) & 1][32 * c + 2 * e]);
-                            de = *reinterpret_cast<const float2*>(&sm.delta[group][(i >> 1) & 1][32 * c + 2 * e]);
+                        if (KEYS && (e & 1) == 0) {
+                            ls = *reinterpret_cast<const float4*>(&sm.stat[s][0][32 * c + 2 * e]);
+                            de = *reinterpret_cast<const float4*>(&sm.stat[s][1][32 * c + 2 * e]);
                         }
-                        fma2(__uint_as_float(sv[2 * e]), __uint_as_float(sv[2 * e + 1]), p.scale2, ls.x, ls.y, x0, x1);
+                        fma2(__uint_as_float(sv[2 * e]), __uint_as_float(sv[2 * e + 1]), p.scale2, e & 1 ? ls.z : ls.x, e & 1 ? ls.w : ls.y,
+                             x0, x1);
                         x0 = ex2_approx(x0);
                         x1 = ex2_approx(x1);
-                        add2(g0, g1, de.x, de.y);
+                        add2(g0, g1, e & 1 ? de.z : de.x, e & 1 ? de.w : de.y);
                         mul2_pair(g0, g1, x0, x1);
+                        if (!KEYS) {
+                            if (!all) {
+                                if (!((bits >> (2 * e)) & 1u)) g0 = 0.0f;
+                                if (!((bits >> (2 * e + 1)) & 1u)) g1 = 0.0f;
+                            }
+                            add2(rest[(e & 1) * 2], rest[(e & 1) * 2 + 1], g0, g1);
+                        }
                         pp[e] = pack_bf16(x0, x1);
                         pd[e] = pack_bf16(g0, g1);
                     }
-                    if (!all) {          // (what is masked may be NaN: its bits go)
-                        const uint32_t bits = r >= len ? 0u : KEYS ? bit_range(r - s0, min(r + p.window - 1, len - 1) - s0)
-                                                                   : seen_bits(r, s0, p.window, p.sinks, len);
+                    if (!all)
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
                             const uint32_t keep = ((bits >> (2 * e)) & 1u ? 0x0000ffffu : 0u) | ((bits >> (2 * e + 1)) & 1u ? 0xffff0000u : 0u);
                             pp[e] &= keep;
                             pd[e] &= keep;
                         }
-                    }
                 } else {
+                    tc_fence_before();
+                    mbar_arrive(&sm.s_free[group]);
 #pragma unroll
                     for (int e = 0; e < 16; ++e) pp[e] = pd[e] = 0u;
                 }
-                // over the columns that this thread has read
-                if (KEYS) tmem_st16(at_s + 32 * c, pp);
-                tmem_st16(at_dp + 32 * c, pd);
+                // The columns of P and dS serve both groups in turn: the products of the tile before, the other
+                // group's, have been made.  (That group waits for these before its next ones, so neither can be two
+                // phases ahead.)
+                if (i > 0 && !(ok = warp_wait(&sm.p_free[group ^ 1], ((i - 1) >> 1) & 1, limit, abort_flag, p.status))) break;
+                tc_fence_after();
+                tmem_st16(lanes + kColP + 16 * c, pp);
+                tmem_st16(lanes + kColDS + 16 * c, pd);
             }
             // rows past the sequence's end do not count, whatever they hold
             if (len < p.T && c0 + kCols > len) {
@@ -324,9 +358,19 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
             tc_fence_before();
             mbar_arrive(&sm.p_ready[group]);
         }
+        float r_sum = 0.0f;
+        if (!KEYS && ok && n > 0) {
+            sm.rest[2 * group + c][row] = (rest[0] + rest[1]) + (rest[2] + rest[3]);
+            mbar_arrive(&sm.r_ready);
+            ok = warp_wait(&sm.r_ready, 0, limit, abort_flag, p.status);
+            r_sum = (sm.rest[0][row] + sm.rest[1][row]) + (sm.rest[2][row] + sm.rest[3][row]);
+        }
+        // (rows of no sequence get zeros, up to the end of the last block)
+        if (!KEYS && ok && group == 1 && r < (p.T + kCols - 1) / kCols * kCols)
+            p.stat[window_stat_at(p.T, bh, r) + kCols * c] = r >= len ? 0.0f : c == 0 ? row_lse : row_delta - r_sum;
         if (ok && n > 0) ok = warp_wait(&sm.done, 0, limit, abort_flag, p.status);
         tc_fence_after();
-        // group 0: A1 (dK, dQ), times scale; group 1: A2 (dV)
+        // group 0: A1 (dK, dQ - what r takes away), times scale; group 1, keys: A2 (dV)
         if (ok && (KEYS || group == 0)) {
             const float f = group == 0 ? p.scale : 1.0f;
             __nv_bfloat16* out = group == 0 ? p.a1 + b * p.a1s[0] + r * p.a1s[1] + h * p.a1s[2]
@@ -338,6 +382,13 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
                 if (n > 0) {
                     tmem_ld32(lanes + (group == 0 ? kColA1 : kColA2) + 32 * c, a);
                     tmem_wait_ld();
+                    if (!KEYS) {
+                        uint32_t pk[32];
+                        tmem_ld32(lanes + kColA2 + 32 * c, pk);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) a[e] = __float_as_uint(fmaf(-r_sum, __uint_as_float(pk[e]), __uint_as_float(a[e])));
+                    }
                 }
                 const bool live = r < p.T && 32 * c < p.d;
 #pragma unroll
@@ -396,17 +447,18 @@ cudaError_t launch_window_backward_tc(const WindowArgs& a, cudaStream_t st)
     Params p{};
     p.B = a.B, p.T = a.T, p.Hq = a.Hq, p.Hk = a.Hk, p.d = a.d, p.window = a.window, p.sinks = a.sinks;
     p.scale = a.scale, p.scale2 = a.scale * kLog2e;
-    p.lengths = a.lengths, p.lse = a.lse, p.delta = a.ws, p.sums = a.ws + window_delta_floats(a);
+    p.lengths = a.lengths, p.lse = a.lse, p.stat = a.ws, p.sums = a.ws + window_stat_floats(a);
     p.status = a.status, p.wait_limit = a.wait_limit;
     typedef const __nv_bfloat16* in;
     typedef __nv_bfloat16* out;
+    p.x1 = static_cast<in>(a.q), p.x2 = static_cast<in>(a.dout), p.o = static_cast<in>(a.o), p.a1 = static_cast<out>(a.dq);
+    copy3(p.x1s, a.qs), copy3(p.x2s, a.dos), copy3(p.os, a.os), copy3(p.a1s, a.dqs);
+    e = launch_dependent(window_backward_tc_kernel<false>, dim3(tiles * a.B * a.Hq), dim3(kThreads), smem, st, mk, mv, p);
+    if (e != cudaSuccess) return e;
+    if (a.sinks > 0 && a.window < a.T && (e = launch_window_prep(a, false, st)) != cudaSuccess) return e;
     p.x1 = static_cast<in>(a.k), p.x2 = static_cast<in>(a.v), p.a1 = static_cast<out>(a.dk), p.a2 = static_cast<out>(a.dv);
     copy3(p.x1s, a.ks), copy3(p.x2s, a.vs), copy3(p.a1s, a.dks), copy3(p.a2s, a.dvs);
-    e = launch_dependent(window_backward_tc_kernel<true>, dim3(tiles * a.B * a.Hk), dim3(kThreads), smem, st, mq, mg, p);
-    if (e != cudaSuccess) return e;
-    p.x1 = static_cast<in>(a.q), p.x2 = static_cast<in>(a.dout), p.a1 = static_cast<out>(a.dq), p.a2 = nullptr;
-    copy3(p.x1s, a.qs), copy3(p.x2s, a.dos), copy3(p.a1s, a.dqs);
-    return launch_dependent(window_backward_tc_kernel<false>, dim3(tiles * a.B * a.Hq), dim3(kThreads), smem, st, mk, mv, p);
+    return launch_dependent(window_backward_tc_kernel<true>, dim3(tiles * a.B * a.Hk), dim3(kThreads), smem, st, mq, mg, p);
 }
 
 }  // namespace lasad

@@ -55,6 +55,14 @@ __device__ __forceinline__ bool warp_wait(void* bar, unsigned parity, unsigned l
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, limit, abort_flag, status));
 }
 
+// Copies `bytes` (a multiple of 16, both ends on 16 bytes) of this GPU's memory; they count on `bar`.
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, unsigned bytes, void* bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
+                 "l"(src), "r"(bytes), "r"(smem_u32(bar))
+                 : "memory");
+}
+
 // Zeroes one 128-byte row of a tile.
 __device__ __forceinline__ void zero_row(unsigned char* row)
 {

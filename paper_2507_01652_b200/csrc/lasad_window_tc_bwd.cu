@@ -35,6 +35,7 @@
 // group of four warps with 64 columns each left a scheduler two warps, too few to hide the
 // latency of TMEM and of the exponentials).  Warp 16: MMA issue.  Warp 17: TMA.
 #include "lasad_window_tma.cuh"
+#include <type_traits>
 
 namespace lasad {
 namespace {
@@ -156,20 +157,28 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
             n = extra + (min(r0 + kRows, len) + kCols - 1) / kCols - lo;
         }
     }
-    auto first_of = [&](int i) { return (KEYS ? lo + i % per : i < extra ? i : lo + i - extra) * kCols; };
-    auto head_of = [&](int i) { return KEYS ? h * G + i / per : h / G; };
+    // A walk over them: tile i is tile number `at` of head `head`.
+    struct Walk {
+        int at, head;
+    };
+    auto move = [&](Walk& w, int by) {
+        w.at += by;
+        while (KEYS && w.at >= per) w.at -= per, ++w.head;
+    };
+    auto first_of = [&](const Walk& w) { return (KEYS ? lo + w.at : w.at < extra ? w.at : lo + w.at - extra) * kCols; };
 
     if (warp == 17) {
         if (elect_one()) {
             int issued = 0;
-            for (; issued < n; ++issued) {
+            Walk w{0, KEYS ? h * G : h / G};
+            for (; issued < n; ++issued, move(w, 1)) {
                 const int s = issued % kStages;
                 if (issued >= kStages && !mbar_wait(&sm.free[s], (issued / kStages - 1) & 1, limit, abort_flag, p.status)) break;
                 mbar_arrive_expect_tx(&sm.full[s], 2 * kTile + (KEYS ? 8 * kCols : 0));
-                tma_load_4d(sm.y1[s], &tm_y1, &sm.full[s], 0, head_of(issued), first_of(issued), b);
-                tma_load_4d(sm.y2[s], &tm_y2, &sm.full[s], 0, head_of(issued), first_of(issued), b);
+                tma_load_4d(sm.y1[s], &tm_y1, &sm.full[s], 0, w.head, first_of(w), b);
+                tma_load_4d(sm.y2[s], &tm_y2, &sm.full[s], 0, w.head, first_of(w), b);
                 if (KEYS)
-                    bulk_load(sm.stat[s], p.stat + window_stat_at(p.T, (long long)b * p.Hq + head_of(issued), first_of(issued)),
+                    bulk_load(sm.stat[s], p.stat + window_stat_at(p.T, (long long)b * p.Hq + w.head, first_of(w)),
                               8 * kCols, &sm.full[s]);
             }
             // leave only when every issued load has landed
@@ -269,8 +278,10 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
             row_lse = -p.lse[(long long)bh * p.T + r] * kLog2e;
             row_delta = -(sm.part[0][row] + sm.part[1][row]);
         }
-        for (int i = group; ok && i < n; i += 2) {
-            const int s = i % kStages, c0 = first_of(i);
+        Walk at_tile{0, 0};
+        if (n > 0) move(at_tile, group);
+        for (int i = group; ok && i < n; i += 2, move(at_tile, 2)) {
+            const int s = i % kStages, c0 = first_of(at_tile);
             // (the tile's statistics; a group has every other tile, so it sees every phase of its places, and a
             // place's next phase needs this tile's products)
             if (KEYS && !(ok = warp_wait(&sm.full[s], (i / kStages) & 1, limit, abort_flag, p.status))) break;
@@ -295,42 +306,38 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
                     tmem_wait_ld();
                     tc_fence_before();
                     mbar_arrive(&sm.s_free[group]);
-                    // (what is masked may be NaN: its bits go)
-                    uint32_t bits = 0xffffffffu;
-                    if (!all)
-                        bits = r >= len ? 0u : KEYS ? bit_range(r - s0, min(r + p.window - 1, len - 1) - s0)
-                                                    : seen_bits(r, s0, p.window, p.sinks, len);
-                    float4 ls = make_float4(row_lse, row_lse, row_lse, row_lse), de = make_float4(row_delta, row_delta, row_delta, row_delta);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        float x0, x1, g0 = __uint_as_float(dv[2 * e]), g1 = __uint_as_float(dv[2 * e + 1]);
-                        if (KEYS && (e & 1) == 0) {
-                            ls = *reinterpret_cast<const float4*>(&sm.stat[s][0][32 * c + 2 * e]);
-                            de = *reinterpret_cast<const float4*>(&sm.stat[s][1][32 * c + 2 * e]);
-                        }
-                        fma2(__uint_as_float(sv[2 * e]), __uint_as_float(sv[2 * e + 1]), p.scale2, e & 1 ? ls.z : ls.x, e & 1 ? ls.w : ls.y,
-                             x0, x1);
-                        x0 = ex2_approx(x0);
-                        x1 = ex2_approx(x1);
-                        add2(g0, g1, e & 1 ? de.z : de.x, e & 1 ? de.w : de.y);
-                        mul2_pair(g0, g1, x0, x1);
-                        if (!KEYS) {
-                            if (!all) {
-                                if (!((bits >> (2 * e)) & 1u)) g0 = 0.0f;
-                                if (!((bits >> (2 * e + 1)) & 1u)) g1 = 0.0f;
-                            }
-                            add2(rest[(e & 1) * 2], rest[(e & 1) * 2 + 1], g0, g1);
-                        }
-                        pp[e] = pack_bf16(x0, x1);
-                        pd[e] = pack_bf16(g0, g1);
-                    }
-                    if (!all)
+                    // MASKED: not all of the pairs count (what is masked may be NaN: its bits go)
+                    auto elements = [&](auto masked) {
+                        constexpr bool MASKED = decltype(masked)::value;
+                        uint32_t bits = 0xffffffffu;
+                        if (MASKED)
+                            bits = r >= len ? 0u : KEYS ? bit_range(r - s0, min(r + p.window - 1, len - 1) - s0)
+                                                        : seen_bits(r, s0, p.window, p.sinks, len);
+                        float4 ls = make_float4(row_lse, row_lse, row_lse, row_lse), de = make_float4(row_delta, row_delta, row_delta, row_delta);
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
-                            const uint32_t keep = ((bits >> (2 * e)) & 1u ? 0x0000ffffu : 0u) | ((bits >> (2 * e + 1)) & 1u ? 0xffff0000u : 0u);
-                            pp[e] &= keep;
-                            pd[e] &= keep;
+                            float x0, x1, g0 = __uint_as_float(dv[2 * e]), g1 = __uint_as_float(dv[2 * e + 1]);
+                            if (KEYS && (e & 1) == 0) {
+                                ls = *reinterpret_cast<const float4*>(&sm.stat[s][0][32 * c + 2 * e]);
+                                de = *reinterpret_cast<const float4*>(&sm.stat[s][1][32 * c + 2 * e]);
+                            }
+                            fma2(__uint_as_float(sv[2 * e]), __uint_as_float(sv[2 * e + 1]), p.scale2, e & 1 ? ls.z : ls.x,
+                                 e & 1 ? ls.w : ls.y, x0, x1);
+                            x0 = ex2_approx(x0);
+                            x1 = ex2_approx(x1);
+                            add2(g0, g1, e & 1 ? de.z : de.x, e & 1 ? de.w : de.y);
+                            mul2_pair(g0, g1, x0, x1);
+                            if (MASKED) {
+                                if (!((bits >> (2 * e)) & 1u)) x0 = g0 = 0.0f;
+                                if (!((bits >> (2 * e + 1)) & 1u)) x1 = g1 = 0.0f;
+                            }
+                            if (!KEYS) add2(rest[(e & 1) * 2], rest[(e & 1) * 2 + 1], g0, g1);
+                            pp[e] = pack_bf16(x0, x1);
+                            pd[e] = pack_bf16(g0, g1);
                         }
+                    };
+                    if (all) elements(std::false_type{});
+                    else elements(std::true_type{});
                 } else {
                     tc_fence_before();
                     mbar_arrive(&sm.s_free[group]);

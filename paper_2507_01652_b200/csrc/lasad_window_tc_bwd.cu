@@ -54,12 +54,12 @@ struct Smem {
     float stat[kStages][2][kCols];                         // keys: -lse log2(e) and -Delta of the tile's rows
     float part[2][kRows], rest[4][kRows];                  // queries: halves of Delta', quarters of r
     unsigned long long full[kStages], free[kStages];       // Y1 and Y2 have landed; their products have been made
-    unsigned long long x_ready;                            // X1 and X2 are in TMEM, queries: Delta' is in part (2 kGroup arrivals)
+    unsigned long long x_ready;                            // X1 and X2 are in TMEM (2 kGroup arrivals)
     unsigned long long s_full[2];                          // S and dP of a group's tile are there
     unsigned long long s_free[2];                          // ... and have been read (kGroup arrivals)
     unsigned long long p_ready[2];                         // P and dS of a group's tile are there (kGroup arrivals)
     unsigned long long p_free[2];                          // ... and their products have been made
-    unsigned long long r_ready;                            // queries: r is in rest (2 kGroup arrivals)
+    unsigned long long r_ready;                            // queries: Delta' is in part, then r in rest (2 kGroup arrivals)
     unsigned long long done, drain[2];
     uint32_t tmem_base;
     int abort_flag;
@@ -251,32 +251,32 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
         const int row = (warp & 3) * 32 + lane, r = r0 + row, gt = tid & (kGroup - 1);
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const int rw0 = r0 + (warp & 3) * 32, rw1 = rw0 + 31;     // the warp's rows
-        // X1 by group 0, X2 by group 1, half a row each
+        // X1 by group 0, X2 by group 1, half a row each (all loads first: they are in flight together)
         const bool mine = r < len && 32 * c < p.d;
-        {
-            const __nv_bfloat16* x = group == 0 ? p.x1 + b * p.x1s[0] + r * p.x1s[1] + h * p.x1s[2]
-                                                : p.x2 + b * p.x2s[0] + r * p.x2s[1] + h * p.x2s[2];
-            uint32_t xv[16];
-            half_row(x + 32 * c, mine, xv);
-            tmem_st16(lanes + (group == 0 ? kColX1 : kColX2) + 16 * c, xv);
-            if (!KEYS && group == 1) {
-                uint32_t ov[16];
-                half_row(p.o + b * p.os[0] + r * p.os[1] + h * p.os[2] + 32 * c, mine, ov);
-                float sum = 0.0f;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) sum = fmaf(bf16_lo(xv[e]), bf16_lo(ov[e]), fmaf(bf16_hi(xv[e]), bf16_hi(ov[e]), sum));
-                sm.part[c][row] = sum;
-            }
+        uint32_t xv[16], ov[16];
+        half_row((group == 0 ? p.x1 + b * p.x1s[0] + r * p.x1s[1] + h * p.x1s[2]
+                             : p.x2 + b * p.x2s[0] + r * p.x2s[1] + h * p.x2s[2]) + 32 * c, mine, xv);
+        float row_lse = 0.0f, row_delta = 0.0f, rest[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (!KEYS) {
+            if (group == 1) half_row(p.o + b * p.os[0] + r * p.os[1] + h * p.os[2] + 32 * c, mine, ov);
+            if (r < len) row_lse = -p.lse[(long long)bh * p.T + r] * kLog2e;
         }
+        tmem_st16(lanes + (group == 0 ? kColX1 : kColX2) + 16 * c, xv);
         tmem_wait_st();
         tc_fence_before();
         mbar_arrive(&sm.x_ready);
 
         bool ok = true;
-        float row_lse = 0.0f, row_delta = 0.0f, rest[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (!KEYS && n > 0 && (ok = warp_wait(&sm.x_ready, 0, limit, abort_flag, p.status)) && r < len) {
-            row_lse = -p.lse[(long long)bh * p.T + r] * kLog2e;
-            row_delta = -(sm.part[0][row] + sm.part[1][row]);
+        if (!KEYS && n > 0) {
+            if (group == 1) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sum = fmaf(bf16_lo(xv[e]), bf16_lo(ov[e]), fmaf(bf16_hi(xv[e]), bf16_hi(ov[e]), sum));
+                sm.part[c][row] = sum;
+            }
+            mbar_arrive(&sm.r_ready);
+            ok = warp_wait(&sm.r_ready, 0, limit, abort_flag, p.status);
+            if (r < len) row_delta = -(sm.part[0][row] + sm.part[1][row]);
         }
         Walk at_tile{0, 0};
         if (n > 0) move(at_tile, group);
@@ -369,7 +369,7 @@ window_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
         if (!KEYS && ok && n > 0) {
             sm.rest[2 * group + c][row] = (rest[0] + rest[1]) + (rest[2] + rest[3]);
             mbar_arrive(&sm.r_ready);
-            ok = warp_wait(&sm.r_ready, 0, limit, abort_flag, p.status);
+            ok = warp_wait(&sm.r_ready, 1, limit, abort_flag, p.status);
             r_sum = (sm.rest[0][row] + sm.rest[1][row]) + (sm.rest[2][row] + sm.rest[3][row]);
         }
         // (rows of no sequence get zeros, up to the end of the last block)

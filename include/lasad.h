@@ -385,7 +385,8 @@ int lasad_qk_norm_rope_backward(lasad_ctx* ctx, const lasad_rope_params* p, cons
  *   h / (Hq / Hk)), 1 <= window, 0 <= sinks <= 128.
  *   lengths [B] int32 (device) or NULL: sequence b ends before token lengths[b] (0 to T).  A row
  *   past the end is empty: its o and gradients are 0 and its lse is -infinity, and nothing that
- *   stands in q, k, v, o, do there counts, not even a NaN.
+ *   stands in q, k, v, o, do there counts, not even a NaN.  (A NaN or an infinity before the end may
+ *   reach rows that do not see it: a weight of 0 times an infinity is not 0.)
  *   lse [B,Hq,T] fp32: log of the row's sum of e^(scale q.k); may be NULL in the forward.
  * With bf16 the products run on the tensor cores with fp32 accumulation, statistics and exponentials
  * in fp32; the weights p and the gradients of the scores are rounded to bf16 where they enter a

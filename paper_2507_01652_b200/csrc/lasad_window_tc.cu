@@ -4,8 +4,7 @@
 //     O += P V (128 x 64 x 64, P from TMEM) ,  l += rowsum(P) ,  o = O / l ,  lse = (m + log2 l) ln 2 .
 //
 // A unit of work is 128 queries of one head, over the visible tiles of 64 keys only: from the
-// window's edge to the diagonal and, where the window has left them, the tiles of the sinks (cut to the
-// 32-column blocks that hold any).  One CTA per SM stays for the whole launch; in it three groups of
+// window's edge to the diagonal and, where the window has left them, the tiles of the sinks.  One CTA per SM stays for the whole launch; in it three groups of
 // warps take units on their own, one after another: four softmax warps and one that issues the
 // products; one more warp asks for the tiles of all three.  One thread has one row, so its maximum and
 // sum need no exchange.  m is a lagging maximum: it moves, and O and l are scaled, only when a row's
@@ -13,12 +12,14 @@
 // the first tiles is rare.  32-column blocks that no row of a warp sees are skipped, and only blocks on
 // an edge are masked.
 //
-// What bounds it: the exponentials, 16 per SM and clock: 512 clocks for a 128 x 64 tile whose
-// products take 320.  What else a tile costs a group (S out of TMEM, the maximum, P into TMEM, the
-// barriers) is latency, 900 clocks of it, and passes under the other groups' exponentials; the products do
-// not add to it, because S, P and O have columns of their own (160 a group, 480 of the SM's 512): the
-// next tile's S is made while this tile's exponentials run.  (Two CTAs of two groups with P over S,
-// so that a tile's products stood between two tiles' exponentials, took 1.7 times as long.)
+// What bounds it: the exponentials, 16 per SM and clock, are 512 clocks for a 128 x 64 tile, and its
+// products 320.  A tile costs each of its group's warps 460 instructions and its group about 2700 clocks, most of
+// them latency (S out of TMEM, the maximum, P into TMEM, the barriers), so that three groups bring
+// one every 900.  S, P and O have columns of their own (160 a group, 480 of the SM's 512): the next
+// tile's S is made while this tile's exponentials run.  Measured: 1 x 9217 tokens, 24 query and 8 key
+// heads, window 1536: 168 us; 64 x 577 tokens, 16 heads, window 144: 137 us.  (Two CTAs of two groups
+// with P over S, so that a tile's products stood between two tiles' exponentials: 170 and 162 us; tiles of
+// 128 keys do not fit the registers: 363 us for the first.)
 //
 // All waits are bounded (see mbar_wait); a wait that gives up sets the status word and the CTA leaves
 // through the normal exit with its copies landed and its TMEM freed.

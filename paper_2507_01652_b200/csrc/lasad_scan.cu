@@ -148,15 +148,16 @@ __device__ __forceinline__ void gate_of(num<VEC> z, num<VEC>& lam, num<VEC>& res
     }
 }
 
-// Which of a slot's kTok tokens end a grid row, for slots that are visited a chunk further on, or
+// Which of a slot's kTok tokens end a grid row, for slots that are visited some tokens further on, or
 // back, each time.
 struct RowEnds {
     long long j;         // grid index of the slot's first token (negative before the grid)
-    int w, col, step;    // col = j mod w where j >= 0
-    __device__ __forceinline__ RowEnds(long long i, int grid_w, int prefix_len) : j(i - prefix_len), w(grid_w), col(0), step(0)
+    int w, by, col, step;    // col = j mod w where j >= 0; by: tokens to the next visit
+    __device__ __forceinline__ RowEnds(long long i, int grid_w, int prefix_len, int tokens)
+        : j(i - prefix_len), w(grid_w), by(tokens), col(0), step(0)
     {
         if (w > 0) {
-            step = kScanChunk % w;
+            step = by % w;
             if (j >= 0) col = (int)(j % w);
         }
     }
@@ -171,7 +172,7 @@ struct RowEnds {
     __device__ __forceinline__ void forward()
     {
         const bool on = j >= 0;
-        j += kScanChunk;
+        j += by;
         if (w <= 0) return;
         if (on) {
             col += step;
@@ -182,7 +183,7 @@ struct RowEnds {
     }
     __device__ __forceinline__ void back()
     {
-        j -= kScanChunk;
+        j -= by;
         if (w <= 0 || j < 0) return;
         col -= step;
         if (col < 0) col += w;
@@ -238,9 +239,11 @@ struct Stage {
     const T* src[NA];        // WIDE: the lane's first piece of the warp's first row; else the lane's channels there
     long long stride[NA];
     int row, piece;          // WIDE: of the lane's first copy
+    int gap;                 // tokens from a slot to the next
     bool in;
-    __device__ __forceinline__ Stage(unsigned char* m, int lane32, int warp) : mem(m)
+    __device__ __forceinline__ Stage(unsigned char* m, int lane32, int warp, int g) : mem(m), gap(g)
     {
+        static_assert(kTok % (32 / kPieces) == 0 || !WIDE, "");
         row = lane32 / kPieces;
         piece = lane32 % kPieces;
         mem += warp * (32 / LC) * kSlot;
@@ -255,7 +258,7 @@ struct Stage {
             src[n] = static_cast<const T*>(base) + row * str + c;
             in = c_tile + c < C;
         } else {
-            src[n] = static_cast<const T*>(base) + sub * kTok * str + lane * VEC;
+            src[n] = static_cast<const T*>(base) + (long long)sub * gap * str + lane * VEC;
             in = c_tile + lane * VEC < C;
         }
     }
@@ -268,26 +271,26 @@ struct Stage {
             if (WIDE) {
 #pragma unroll
                 for (int k = 0; k < kCopies; ++k) {
-                    const int r = row + k * (32 / kPieces);
-                    const bool live = in && r < rows;
-                    const uint32_t dst = tcx::smem_u32(to + (r / kTok) * kSlot + (r % kTok) * kRow + piece * 16);
-                    const T* from = live ? src[n] + (long long)(k * (32 / kPieces)) * stride[n] : src[n];
+                    const int slot = k * (32 / kPieces) / kTok, t = k * (32 / kPieces) % kTok, at = slot * gap + t;
+                    const bool live = in && row + at < rows;
+                    const uint32_t dst = tcx::smem_u32(to + slot * kSlot + (row + t) * kRow + piece * 16);
+                    const T* from = live ? src[n] + at * stride[n] : src[n];
                     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(from), "r"(live ? 16 : 0) : "memory");
                 }
             } else {
                 const int lane = threadIdx.x % LC, sub = (threadIdx.x & 31) / LC;
 #pragma unroll
                 for (int t = 0; t < kTok; ++t)
-                    if (in && sub * kTok + t < rows)
+                    if (in && sub * gap + t < rows)
                         reinterpret_cast<raw*>(to + sub * kSlot + t * kRow)[lane] = *reinterpret_cast<const raw*>(src[n] + t * stride[n]);
             }
         }
         if (WIDE) asm volatile("cp.async.commit_group;" ::: "memory");
     }
-    __device__ __forceinline__ void move(int chunks)
+    __device__ __forceinline__ void move(int tokens)
     {
 #pragma unroll
-        for (int n = 0; n < NA; ++n) src[n] += chunks * kScanChunk * stride[n];
+        for (int n = 0; n < NA; ++n) src[n] += tokens * stride[n];
     }
     __device__ __forceinline__ void landed(bool last)
     {
@@ -306,7 +309,8 @@ struct Stage {
 };
 
 // LC lanes of VEC channels make a tile; a CTA has LC * kSlots threads.
-// SUMMARY: only (A, H) of a whole segment.
+// SUMMARY: only (A, H) of a whole segment.  A slot then has a run of the segment's tokens, not a part of every
+// chunk, and the slots meet once at the end.
 template <typename T, int VEC, int LC, bool WIDE, bool LOGITS, bool TIED, bool SUMMARY>
 __global__ void __launch_bounds__(LC * kSlots, LC == 16 ? 3 : 1) scan_forward_kernel(const ScanArgs a)
 {
@@ -322,13 +326,14 @@ __global__ void __launch_bounds__(LC * kSlots, LC == 16 ? 3 : 1) scan_forward_ke
     const Work wk(a, SUMMARY ? 0 : -1, chunks, LC * VEC);
     const int b = wk.b, tile0 = wk.c, c0 = tile0 + lane * VEC, first = wk.first, end = wk.end;
     const bool in = c0 < a.C;                      // (VEC = 2 only where C is even)
-    const int w0 = first * kScanChunk + warp * (32 / LC) * kTok, t0 = first * kScanChunk + slot * kTok;
-    Stage<T, VEC, LC, 2, WIDE> st(mem, threadIdx.x & 31, warp);
+    const int run = SUMMARY ? (end - first) * kTok : kTok, by = SUMMARY ? kTok : kScanChunk;   // a slot's tokens; to its next visit
+    const int w0 = first * kScanChunk + warp * (32 / LC) * run, t0 = first * kScanChunk + slot * run;
+    Stage<T, VEC, LC, 2, WIDE> st(mem, threadIdx.x & 31, warp, run);
     st.tensor(0, static_cast<const T*>(a.x) + b * a.xs[0] + tile0 + w0 * a.xs[1], a.xs[1], tile0, a.C);
     st.tensor(1, static_cast<const T*>(a.gate) + b * a.gs[0] + tile0 + w0 * a.gs[1], a.gs[1], tile0, a.C);
     T* y = static_cast<T*>(a.y) + b * a.ys[0] + c0 + t0 * a.ys[1];
     const long long state = (long long)b * a.C + c0;
-    RowEnds rows(a.t0 + t0, a.grid_w, a.prefix_len);
+    RowEnds rows(a.t0 + t0, a.grid_w, a.prefix_len, by);
     int rest_rows = a.T - w0, left = a.T - t0;     // tokens from the warp's, the slot's first one to the end
     pdl_wait();
     st.fetch(first & 1, rest_rows);
@@ -346,8 +351,9 @@ __global__ void __launch_bounds__(LC * kSlots, LC == 16 ? 3 : 1) scan_forward_ke
         const int buf = chunk & 1;
         // the next chunk comes in under this one's arithmetic (its buffer was read before the last barrier)
         if (chunk + 1 < end) {
-            st.move(1);
-            st.fetch(buf ^ 1, rest_rows - kScanChunk);
+            if (SUMMARY) __syncwarp();             // (there is no barrier: the warp's own lanes have read it)
+            st.move(by);
+            st.fetch(buf ^ 1, rest_rows - by);
         }
         st.landed(chunk + 1 == end);
         N ca[kTok], cb[kTok];
@@ -373,42 +379,54 @@ __global__ void __launch_bounds__(LC * kSlots, LC == 16 ? 3 : 1) scan_forward_ke
             A = A * ca[t];
             H = fma(ca[t], H, cb[t]);
         }
+        if constexpr (SUMMARY) {
+            h0 = fma(A, h0, H);
+            total = total * A;
+            rest_rows -= by;
+            left -= by;
+            rows.forward();
+            continue;
+        }
         span[buf][slot][lane] = {A, H};
         __syncthreads();
         // h before this slot (the chunk's own start came through `next` at the same barrier)
         N h = chunk == first ? h0 : next[buf][lane];
-        if (!SUMMARY && slot == 0 && a.saved && in)
+        if (slot == 0 && a.saved && in)
             store_state<VEC>(a.saved + ((long long)b * chunks + chunk) * a.C + c0, h);
 #pragma unroll 5
         for (int s = 0; s < slot; ++s) {
             const Span m = span[buf][s][lane];
             h = fma(m.A, h, m.H);
-            if (SUMMARY && slot == kSlots - 1) total = total * m.A;
         }
         if (slot == kSlots - 1) {
             const N after = fma(A, h, H);
-            if (SUMMARY) total = total * A;
             next[buf ^ 1][lane] = after;
-            if (chunk == end - 1 && in) {
-                if (SUMMARY) {
-                    float* w = wk.span(a, wk.seg) + lane * VEC;
-                    store_state<VEC>(w, total);
-                    store_state<VEC>(w + LC * VEC, after);
-                } else if (end == chunks && a.h_out) {
-                    store_state<VEC>(a.h_out + state, after);
-                }
-            }
+            if (chunk == chunks - 1 && in && a.h_out) store_state<VEC>(a.h_out + state, after);
         }
-        if (!SUMMARY && in)
+        if (in)
 #pragma unroll
             for (int t = 0; t < kTok; ++t) {
                 h = fma(ca[t], h, cb[t]);
                 if (t < left) *reinterpret_cast<raw*>(y + t * a.ys[1]) = P::put(h);
             }
         y += kScanChunk * a.ys[1];
-        rest_rows -= kScanChunk;
-        left -= kScanChunk;
+        rest_rows -= by;
+        left -= by;
         rows.forward();
+    }
+    if constexpr (SUMMARY) {
+        span[0][slot][lane] = {total, h0};
+        __syncthreads();
+        if (slot == 0 && in) {
+            for (int s = 1; s < kSlots; ++s) {
+                const Span m = span[0][s][lane];
+                h0 = fma(m.A, h0, m.H);
+                total = total * m.A;
+            }
+            float* w = wk.span(a, wk.seg) + lane * VEC;
+            store_state<VEC>(w, total);
+            store_state<VEC>(w + LC * VEC, h0);
+        }
     }
 }
 
@@ -431,8 +449,10 @@ __global__ void __launch_bounds__(LC * kSlots, LC != 16 ? 1 : sizeof(T) == 2 ? 2
     const Work wk(a, SUMMARY ? 1 : -1, chunks, LC * VEC);       // (nothing comes before segment 0: it needs no summary)
     const int b = wk.b, tile0 = wk.c, c0 = tile0 + lane * VEC, first = wk.first, end = wk.end;
     const bool in = c0 < a.C;
-    const int w0 = (end - 1) * kScanChunk + warp * (32 / LC) * kTok, t0 = (end - 1) * kScanChunk + slot * kTok;
-    Stage<T, VEC, LC, SUMMARY ? 2 : 3, WIDE> st(mem, threadIdx.x & 31, warp);
+    const int run = SUMMARY ? (end - first) * kTok : kTok, by = SUMMARY ? kTok : kScanChunk;
+    const int last = SUMMARY ? first * kScanChunk + run - kTok : (end - 1) * kScanChunk;       // slot 0's first visit
+    const int w0 = last + warp * (32 / LC) * run, t0 = last + slot * run;
+    Stage<T, VEC, LC, SUMMARY ? 2 : 3, WIDE> st(mem, threadIdx.x & 31, warp, run);
     st.tensor(0, static_cast<const T*>(a.gate) + b * a.gs[0] + tile0 + w0 * a.gs[1], a.gs[1], tile0, a.C);
     st.tensor(1, static_cast<const T*>(a.dy) + b * a.ys[0] + tile0 + w0 * a.ys[1], a.ys[1], tile0, a.C);
     if constexpr (!SUMMARY) st.tensor(2, static_cast<const T*>(a.x) + b * a.xs[0] + tile0 + w0 * a.xs[1], a.xs[1], tile0, a.C);
@@ -440,7 +460,7 @@ __global__ void __launch_bounds__(LC * kSlots, LC != 16 ? 1 : sizeof(T) == 2 ? 2
     T* dg = static_cast<T*>(a.dgate) + b * a.dgs[0] + c0 + t0 * a.dgs[1];
     const float* saved = a.saved + ((long long)b * chunks + end - 1) * a.C + c0;
     const long long state = (long long)b * a.C + c0;
-    RowEnds rows(a.t0 + t0, a.grid_w, a.prefix_len);
+    RowEnds rows(a.t0 + t0, a.grid_w, a.prefix_len, by);
     int rest_rows = a.T - w0, left = a.T - t0;
     pdl_wait();
     st.fetch((end - 1) & 1, rest_rows);
@@ -459,8 +479,8 @@ __global__ void __launch_bounds__(LC * kSlots, LC != 16 ? 1 : sizeof(T) == 2 ? 2
         N h = hs;
         if (chunk > first) {
             __syncwarp();                          // (dy of the chunk before this one has been read)
-            st.move(-1);
-            st.fetch(buf ^ 1, rest_rows + kScanChunk);
+            st.move(-by);
+            st.fetch(buf ^ 1, rest_rows + by);
             saved -= a.C;
             if (!SUMMARY && in) hs = load_state<VEC>(saved);
         }
@@ -492,6 +512,14 @@ __global__ void __launch_bounds__(LC * kSlots, LC != 16 ? 1 : sizeof(T) == 2 ? 2
             for (int t = 0; t < kTok; ++t) H = fma(ca[t], H, TIED ? rest[t] * xv[t] : xv[t]);
 #pragma unroll
         for (int t = kTok - 1; t >= 0; --t) Q = ca[t] * (Q + grad(t));
+        if constexpr (SUMMARY) {
+            u0 = fma(A, u0, Q);
+            total = total * A;
+            rest_rows += by;
+            left += by;
+            rows.back();
+            continue;
+        }
         back[buf][slot][lane] = {A, Q};
         if (!SUMMARY) fwd[buf][slot][lane] = H;
         __syncthreads();
@@ -500,24 +528,14 @@ __global__ void __launch_bounds__(LC * kSlots, LC != 16 ? 1 : sizeof(T) == 2 ? 2
         for (int s = kSlots - 1; s > slot; --s) {
             const Span m = back[buf][s][lane];
             u = fma(m.A, u, m.X);
-            if (SUMMARY && slot == 0) total = total * m.A;
         }
         if (!SUMMARY)
 #pragma unroll 5
             for (int s = 0; s < slot; ++s) h = fma(back[buf][s][lane].A, h, fwd[buf][s][lane]);
         if (slot == 0) {
             const N before = fma(A, u, Q);
-            if (SUMMARY) total = total * A;
             next[buf ^ 1][lane] = before;
-            if (chunk == first && in) {
-                if (SUMMARY) {
-                    float* w = wk.span(a, wk.seg) + lane * VEC;
-                    store_state<VEC>(w, total);
-                    store_state<VEC>(w + LC * VEC, before);
-                } else if (first == 0 && a.dh_in) {
-                    store_state<VEC>(a.dh_in + state, before);
-                }
-            }
+            if (chunk == 0 && in && a.dh_in) store_state<VEC>(a.dh_in + state, before);
         }
         if constexpr (!SUMMARY) {
             // dlambda_t = g_t f_t, f_t = h_{t-1} - x_t (tied): f_t takes x_t's place
@@ -549,9 +567,23 @@ __global__ void __launch_bounds__(LC * kSlots, LC != 16 ? 1 : sizeof(T) == 2 ? 2
             dx -= kScanChunk * a.dxs[1];
             dg -= kScanChunk * a.dgs[1];
         }
-        rest_rows += kScanChunk;
-        left += kScanChunk;
+        rest_rows += by;
+        left += by;
         rows.back();
+    }
+    if constexpr (SUMMARY) {
+        back[0][slot][lane] = {total, u0};
+        __syncthreads();
+        if (slot == kSlots - 1 && in) {
+            for (int s = kSlots - 2; s >= 0; --s) {
+                const Span m = back[0][s][lane];
+                u0 = fma(m.A, u0, m.X);
+                total = total * m.A;
+            }
+            float* w = wk.span(a, wk.seg) + lane * VEC;
+            store_state<VEC>(w, total);
+            store_state<VEC>(w + LC * VEC, u0);
+        }
     }
 }
 

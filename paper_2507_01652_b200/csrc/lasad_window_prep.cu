@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(32 * kWarps) window_prep_kernel(const WindowAr
     if (DELTA) __syncthreads();                                     // what the CTA's rows have left
     float* sums = a.ws + window_stat_floats(a) + ((long long)bh * chunks + chunk) * sinks * 2 * D;
     constexpr float kLog2e = 1.4426950408889634f;
-    for (int s = 0; s < sinks; ++s) {
+    for (int s = blockIdx.y; s < sinks; s += gridDim.y) {
         float kv[N], vv[N], dk[N], dv[N];
         load_piece<T, N>(static_cast<const T*>(a.k) + b * a.ks[0] + s * a.ks[1] + hk * a.ks[2] + sub * N, kv);
         load_piece<T, N>(static_cast<const T*>(a.v) + b * a.vs[0] + s * a.vs[1] + hk * a.vs[2] + sub * N, vv);
@@ -138,7 +138,8 @@ template <bool DELTA> cudaError_t launch_prep(const WindowArgs& a, cudaStream_t 
     const unsigned n = (unsigned)((a.T + kPrepRows - 1) / kPrepRows) * a.B * a.Hk;
     auto kernel = a.bf16 ? (a.d == 64 ? window_prep_kernel<__nv_bfloat16, 64, DELTA> : window_prep_kernel<__nv_bfloat16, 32, DELTA>)
                          : (a.d == 64 ? window_prep_kernel<float, 64, DELTA> : window_prep_kernel<float, 32, DELTA>);
-    return launch_dependent(kernel, dim3(n), dim3(32 * kWarps), 0, st, a);
+    // (the sums alone: a CTA per sink as well; with Delta the CTA that has formed it goes over all sinks)
+    return launch_dependent(kernel, dim3(n, DELTA ? 1 : (unsigned)(a.sinks < a.T ? a.sinks : a.T)), dim3(32 * kWarps), 0, st, a);
 }
 
 }  // namespace

@@ -377,6 +377,18 @@ def test_window_long_ragged_against_the_other_implementation_and_repeats(ctx, dt
         assert torch.equal(a, b) and torch.equal(a[1:2], c)
 
 
+@pytest.mark.parametrize("T,win", [(2, 8), (40, 2), (300, 2)])
+def test_window_gradient_where_rows_see_two_keys(ctx, T, win):
+    """dP - Delta is small there against Delta itself, which the rounding of o must not reach: dq and dk within
+    2^-8 in the 2-norm (2^-9 and less each from the output, P and dS; Delta from the bf16 o alone: 0.4 to 0.7 %)."""
+    (q, k, v, do), dev = window_case(64, T, 4, 4, 64, BF16, None, 11)
+    leaves = [d64(t).requires_grad_() for t in (q, k, v)]
+    want = torch.autograd.grad(ref.window(*leaves, win)[0], leaves, d64(do))
+    o, lse = ctx.lasad_window_attention(*dev[:3], win, want_lse=True)
+    for a, b in zip(ctx.lasad_window_attention_backward(*dev[:3], o, lse, dev[3], win), want):
+        assert (d64(a) - b).norm() <= 2.0 ** -8 * b.norm()
+
+
 def test_window_back_to_back_in_a_warm_cache(ctx):
     """A long case over and over: tiles land at once, so that every wait meets the barrier's phase that
     is the hardest to tell from the next; no wait may give up, and every launch returns the same bits."""

@@ -308,6 +308,16 @@ struct Stage {
     }
 };
 
+// The wait for the launch before.  The next launch is let in early only by a summary whose launch behind it
+// has no whole tiles: CTAs that come while others still run spread over the SMs as places fall free, and the
+// whole walk then goes at the pace of the fullest SM (4 x 2304 x 1536 forward after itself 34 against 29 us, 10
+// x 2304 x 1536, cut in its last round, 61 against 47).
+template <bool SUMMARY> __device__ __forceinline__ void wait_for(const ScanArgs& a)
+{
+    if (SUMMARY && a.whole == 0) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 // LC lanes of VEC channels make a tile; a CTA has LC * kSlots threads.
 // SUMMARY: only (A, H) of a whole segment.  A slot then has a run of the segment's tokens, not a part of every
 // chunk, and the slots meet once at the end.
@@ -335,7 +345,7 @@ __global__ void __launch_bounds__(LC * kSlots, LC == 16 ? 3 : 1) scan_forward_ke
     const long long state = (long long)b * a.C + c0;
     RowEnds rows(a.t0 + t0, a.grid_w, a.prefix_len, by);
     int rest_rows = a.T - w0, left = a.T - t0;     // tokens from the warp's, the slot's first one to the end
-    pdl_wait();
+    wait_for<SUMMARY>(a);
     st.fetch(first & 1, rest_rows);
     // the state at the segment's first token: h_in through the segments before it
     N h0 = N::all(0.0f), total = N::all(1.0f);
@@ -462,7 +472,7 @@ __global__ void __launch_bounds__(LC * kSlots, LC != 16 ? 1 : sizeof(T) == 2 ? 2
     const long long state = (long long)b * a.C + c0;
     RowEnds rows(a.t0 + t0, a.grid_w, a.prefix_len, by);
     int rest_rows = a.T - w0, left = a.T - t0;
-    pdl_wait();
+    wait_for<SUMMARY>(a);
     st.fetch((end - 1) & 1, rest_rows);
     N u0 = N::all(0.0f), total = N::all(1.0f), hs = N::all(0.0f);      // hs: h before the chunk
     if (!SUMMARY && in) {

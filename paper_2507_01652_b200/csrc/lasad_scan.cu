@@ -692,12 +692,12 @@ cudaError_t launch(const ScanArgs& a, cudaStream_t st)
 // A segment's summary reads two streams once more, of the forward's three and the backward's five, in a
 // launch before, so a cut has to bring three CTAs in the place of one (backward: two).
 //   - So few tiles, and eight chunks or more: all are cut, into as many segments as there are slots for.  Cut
-//     against whole, us, bf16, forward and gradient: 1 x 9217 x 1536 38 and 61 against 89 and 138, 1 x 1024 x 1536 7.5
-//     and 12.1 against 11.1 and 16.5.  Two segments: 4 x 2304 x 1536 forward 37 against 34, 3 x 2304 x 1536 gradient 43
+//     against whole, us, bf16, forward and gradient: 1 x 9217 x 1536 33 and 51 against 89 and 138, 1 x 1024 x 1536 7.5
+//     and 12.1 against 11.1 and 16.5.  Two segments: 4 x 2304 x 1536 forward 37 against 34, 3 x 2304 x 1536 gradient 39
 //     against 48.  Four chunks (1 x 512 x 1536): 6.5 and 7.8 against 6.2 and 8.9.
 //   - A last round of tiles that leaves a quarter of the SMs or more idle: that round is cut.  Gradient of 8 x
-//     2304 x 1536 (88 of 384 tiles) 80 against 82 us, forward in fp32 63 against 67; gradient of 4 x 2304 x 1536 in fp32
-//     (44 of 192) 64 against 80; with 132 of 576 left (12 x 2304 x 1536, forward) 63 against 57.
+//     2304 x 1536 (88 of 384 tiles) 75 against 82 us, forward in fp32 60 against 67; gradient of 4 x 2304 x 1536 in fp32
+//     (44 of 192) 61 against 80; with 132 of 576 left (12 x 2304 x 1536, forward) 63 against 57.
 void scan_plan(ScanArgs& a, bool backward, int sms)
 {
     const long long tiles = (long long)a.B * ((a.C + 31) / 32);

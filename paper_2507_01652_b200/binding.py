@@ -14,7 +14,7 @@ import torch
 
 from . import build as _build
 from . import mixers as _mixers
-from .marshal import (LASAD_BF16, LASAD_F32, _check_cuda, _dtype_code, _ptr, _raw_stream, _stream,  # noqa: F401
+from .marshal import (LASAD_BF16, LASAD_F32, _check_cuda, _dtype_code, _empty, _ptr, _raw_stream, _stream,  # noqa: F401
                       _strides3, _strides_decode)
 from .mixers import rope_table  # noqa: F401
 
@@ -200,9 +200,9 @@ class Lasad(_mixers.Mixers):
         B, T, H, dk = q.shape
         dv = v.shape[3]
         if o is None:
-            o = torch.empty((B, T, H, dv), dtype=q.dtype, device=q.device)
+            o = _empty((B, T, H, dv), q.dtype, q.device, stream)
         if state_out is None and want_state:
-            state_out = torch.empty((B, H, dk, dv), dtype=torch.float32, device=q.device)
+            state_out = _empty((B, H, dk, dv), torch.float32, q.device, stream)
         p = _params("prefill", q, k, v, o, grid_w, prefix_len, t0, scale)
         rc = self._lib.lasad_forward(self._h, ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v),
                                      _ptr(decay), _ptr(state_in), _ptr(o), _ptr(state_out),
@@ -239,7 +239,7 @@ class Lasad(_mixers.Mixers):
         B, H, dk = q.shape
         dv = v.shape[2]
         if o is None:
-            o = torch.empty((B, H, dv), dtype=q.dtype, device=q.device)
+            o = _empty((B, H, dv), q.dtype, q.device, stream)
         if state.dtype != torch.float32 or not state.is_contiguous() or tuple(state.shape) != (B, H, dk, dv):
             raise ValueError("state must be contiguous float32 [B,H,dk,dv]")
         p = _params("decode", q, k, v, o, grid_w, prefix_len, t, scale)
@@ -257,9 +257,9 @@ class Lasad(_mixers.Mixers):
         B, T, H, dk = q.shape
         dv = v.shape[3]
         if o is None:
-            o = torch.empty((B, T, H, dv), dtype=q.dtype, device=q.device)
+            o = _empty((B, T, H, dv), q.dtype, q.device, stream)
         if state_out is None and want_state:
-            state_out = torch.empty((B, H, dk, dv), dtype=torch.float32, device=q.device)
+            state_out = _empty((B, H, dk, dv), torch.float32, q.device, stream)
         if gate.dtype != q.dtype or tuple(gate.shape) != tuple(q.shape):
             raise ValueError("gate must have q's shape and dtype")
         if k is not None and tuple(k.stride()) != tuple(gate.stride()):
@@ -279,7 +279,7 @@ class Lasad(_mixers.Mixers):
         B, H, dk = q.shape
         dv = v.shape[2]
         if o is None:
-            o = torch.empty((B, H, dv), dtype=q.dtype, device=q.device)
+            o = _empty((B, H, dv), q.dtype, q.device, stream)
         if state.dtype != torch.float32 or not state.is_contiguous() or tuple(state.shape) != (B, H, dk, dv):
             raise ValueError("state must be contiguous float32 [B,H,dk,dv]")
         if gate.dtype != q.dtype or tuple(gate.shape) != tuple(q.shape):
@@ -303,7 +303,7 @@ class Lasad(_mixers.Mixers):
         B, H, dk = q.shape
         dv = v.shape[2]
         if o is None:
-            o = torch.empty((B, H, dv), dtype=q.dtype, device=q.device)
+            o = _empty((B, H, dv), q.dtype, q.device, stream)
         if state.dtype != torch.float32 or not state.is_contiguous() or tuple(state.shape) != (B, H, dk, dv):
             raise ValueError("state must be contiguous float32 [B,H,dk,dv]")
         for t in (pos, widths):
@@ -326,9 +326,9 @@ class Lasad(_mixers.Mixers):
         B, T, H, dk = q_pre.shape
         dv = v.shape[3]
         if o is None:
-            o = torch.empty((B, T, H, dv), dtype=q_pre.dtype, device=q_pre.device)
+            o = _empty((B, T, H, dv), q_pre.dtype, q_pre.device, stream)
         if state_out is None and want_state:
-            state_out = torch.empty((B, H, dk, dv), dtype=torch.float32, device=q_pre.device)
+            state_out = _empty((B, H, dk, dv), torch.float32, q_pre.device, stream)
         if gate_pre.dtype != q_pre.dtype or tuple(gate_pre.shape) != tuple(q_pre.shape):
             raise ValueError("gate_pre must have q_pre's shape and dtype")
         if k is not None and tuple(k.stride()) != tuple(gate_pre.stride()):
@@ -351,7 +351,7 @@ class Lasad(_mixers.Mixers):
         B, H, dk = q_pre.shape
         dv = v.shape[2]
         if o is None:
-            o = torch.empty((B, H, dv), dtype=q_pre.dtype, device=q_pre.device)
+            o = _empty((B, H, dv), q_pre.dtype, q_pre.device, stream)
         if state.dtype != torch.float32 or not state.is_contiguous() or tuple(state.shape) != (B, H, dk, dv):
             raise ValueError("state must be contiguous float32 [B,H,dk,dv]")
         if gate_pre.dtype != q_pre.dtype or tuple(gate_pre.shape) != tuple(q_pre.shape):

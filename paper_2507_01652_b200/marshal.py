@@ -36,6 +36,22 @@ def _stream(device, stream):
     return torch.cuda.current_stream(device).cuda_stream
 
 
+def _empty(shape, dtype, device, stream, returned=True):
+    """Memory that a call on ``stream`` (a raw handle; None: the current stream) writes.
+
+    The allocator hands a block on as soon as its owner lets go of it, in the order of the stream it belongs
+    to: memory of the current stream may still be in use by what that stream has to do, and memory that
+    another stream has to write must not go back to the current one.  So it is that stream's own.  What is
+    ``returned`` will be read on the current stream, which the allocator then waits for as well."""
+    if stream is None or device.type != "cuda":         # (the call refuses what is not on a GPU)
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(torch.cuda.ExternalStream(getattr(stream, "value", stream) or 0, device=device)):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if returned:
+        t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
 def _check_cuda(*ts):
     for t in ts:
         if t is not None and not t.is_cuda:

@@ -4,8 +4,9 @@
 spatial rule (``lasad_scan_*``), the norm and rotation of queries and keys (``lasad_qk_norm_rope*``)
 and attention over a sliding window with visible first tokens (``lasad_window_*``).  Gradients are
 explicit calls; outputs that are not passed in are allocated.  Every call is asynchronous on
-``stream`` (a raw handle; the current one by default).  Workspaces come from torch's allocator and
-are its again once the stream has passed the call.
+``stream`` (a raw handle; the current one by default), and what a call allocates belongs to that
+stream: a workspace is free again once the stream has passed the call, an output once the current stream
+too has passed the point where it was dropped.
 """
 from __future__ import annotations
 
@@ -14,7 +15,7 @@ import math
 
 import torch
 
-from .marshal import _check_cuda, _dtype_code, _ptr, _stream, _strides3, _strides_decode
+from .marshal import _check_cuda, _dtype_code, _empty, _ptr, _stream, _strides3, _strides_decode
 
 LASAD_SCAN_TIED = 1
 LASAD_SCAN_LOGITS = 2
@@ -80,9 +81,9 @@ def _look(t):
     return None if t is None else (t.shape, t.stride(), t.dtype, t.is_cuda)
 
 
-def _like(t):
+def _like(t, stream):
     """An output of t's shape, with contiguous channels."""
-    return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+    return torch.empty_like(t) if stream is None and t.is_contiguous() else _empty(t.shape, t.dtype, t.device, stream)
 
 
 class _Entry:
@@ -143,10 +144,7 @@ class Mixers:
             return given
         if not e.ws:
             return None
-        ws = torch.empty(e.ws, dtype=torch.uint8, device=like.device)
-        if stream is not None:       # not handed out again before that stream has passed the call
-            ws.record_stream(torch.cuda.ExternalStream(stream, device=like.device))
-        return ws
+        return _empty(e.ws, torch.uint8, like.device, stream, returned=False)
 
     # ---- gated linear recurrence ------------------------------------------------------------
     def _scan(self, key, kind, x, gate, y, dx, dgate, states, saved, pos):
@@ -175,14 +173,14 @@ class Mixers:
         ``gate`` holds lambda, or with ``logits`` its pre-activation; ``tied`` scales x by 1 - lambda.
         ``save`` keeps the states that ``lasad_scan_backward`` needs."""
         if y is None:
-            y = _like(x)
+            y = _like(x, stream)
         key = ("scan", _look(x), _look(gate), _look(h_in), _look(y), _look(h_out))
         e = self._calls.get(key) or self._scan(key, "forward", x, gate, y, None, None, (("h_in", h_in), ("h_out", h_out)), None, None)
         p = e.p
         self._scan_set(p, grid_w, prefix_len, t0, tied, logits)
         if h_out is None and want_state:
-            h_out = torch.empty((p.B, p.C), dtype=torch.float32, device=x.device)
-        saved = torch.empty((p.B, -(-p.T // LASAD_SCAN_CHUNK), p.C), dtype=torch.float32, device=x.device) if save else None
+            h_out = _empty((p.B, p.C), torch.float32, x.device, stream)
+        saved = _empty((p.B, -(-p.T // LASAD_SCAN_CHUNK), p.C), torch.float32, x.device, stream) if save else None
         ws = self._workspace(e, self._lib.lasad_scan_workspace, x, workspace, stream)
         rc = self._lib.lasad_scan_forward(self._h, e.ref, x.data_ptr(), gate.data_ptr(), _ptr(h_in), y.data_ptr(), _ptr(h_out),
                                           _ptr(saved), _ptr(ws), _stream(x.device, stream))
@@ -194,9 +192,9 @@ class Mixers:
                             dx=None, dgate=None, dh_in=None, want_state=True, workspace=None, stream=None):
         """The gradient of ``lasad_scan_forward``; returns (dx, dgate, dh_in)."""
         if dx is None:
-            dx = _like(x)
+            dx = _like(x, stream)
         if dgate is None:
-            dgate = _like(x)
+            dgate = _like(x, stream)
         key = ("scan'", _look(x), _look(gate), _look(saved), _look(dy), _look(dh_out), _look(dx), _look(dgate),
                _look(dh_in))
         e = self._calls.get(key)
@@ -207,7 +205,7 @@ class Mixers:
         p = e.p
         self._scan_set(p, grid_w, prefix_len, t0, tied, logits)
         if dh_in is None and want_state:
-            dh_in = torch.empty((p.B, p.C), dtype=torch.float32, device=x.device)
+            dh_in = _empty((p.B, p.C), torch.float32, x.device, stream)
         ws = self._workspace(e, self._lib.lasad_scan_workspace, x, workspace, stream)
         rc = self._lib.lasad_scan_backward(self._h, e.ref, x.data_ptr(), gate.data_ptr(), saved.data_ptr(), dy.data_ptr(),
                                            _ptr(dh_out), dx.data_ptr(), dgate.data_ptr(), _ptr(dh_in), _ptr(ws),
@@ -221,7 +219,7 @@ class Mixers:
         """One token of the recurrence, x and gate [B,C]; ``t`` or ``pos`` (int32 [B]) gives its
         position.  The state is updated in place unless ``h_out`` is given.  Returns (y, h_out)."""
         if y is None:
-            y = _like(x)
+            y = _like(x, stream)
         if h_out is None:
             h_out = h_in
         key = ("scan1", _look(x), _look(gate), _look(h_in), _look(y), _look(h_out), _look(pos))
@@ -261,9 +259,9 @@ class Mixers:
         """RMS norm of every head of q [B,T,Hq,d] and k [B,T,Hk,d] and their rotation by position
         (``table`` from ``rope_table``), in one pass; returns (q_out, k_out)."""
         if q_out is None:
-            q_out = _like(q)
+            q_out = _like(q, stream)
         if k_out is None:
-            k_out = _like(k)
+            k_out = _like(k, stream)
         key = ("rope", grid_w > 0, _look(q), _look(k), _look(table), _look(q_weight), _look(k_weight), _look(pos),
                _look(q_out), _look(k_out))
         e = self._calls.get(key) or self._rope(key, q, k, table, q_weight, k_weight, pos, grid_w > 0,
@@ -281,9 +279,9 @@ class Mixers:
         """The gradient of ``lasad_qk_norm_rope`` from its inputs; returns (dq, dk, dq_weight,
         dk_weight), the last two fp32 [d] (None without ``want_weights``)."""
         if dq is None:
-            dq = _like(q)
+            dq = _like(q, stream)
         if dk is None:
-            dk = _like(k)
+            dk = _like(k, stream)
         key = ("rope'", grid_w > 0, _look(q), _look(k), _look(table), _look(q_weight), _look(k_weight), _look(pos),
                _look(dq_out), _look(dk_out), _look(dq), _look(dk))
         e = self._calls.get(key) or self._rope(key, q, k, table, q_weight, k_weight, pos, grid_w > 0,
@@ -291,7 +289,7 @@ class Mixers:
         self._rope_set(e.p, grid_w, prefix_len, t0, half, eps)
         dwq = dwk = ws = None
         if want_weights:
-            dwq, dwk = torch.empty(e.p.d, dtype=torch.float32, device=q.device), torch.empty(e.p.d, dtype=torch.float32, device=q.device)
+            dwq, dwk = _empty(e.p.d, torch.float32, q.device, stream), _empty(e.p.d, torch.float32, q.device, stream)
             ws = self._workspace(e, self._lib.lasad_qk_norm_rope_workspace, q, workspace, stream)
         rc = self._lib.lasad_qk_norm_rope_backward(self._h, e.ref, q.data_ptr(), k.data_ptr(), table.data_ptr(), _ptr(q_weight),
                                                    _ptr(k_weight), _ptr(pos), dq_out.data_ptr(), dk_out.data_ptr(),
@@ -334,13 +332,13 @@ class Mixers:
         1/sqrt(d) by default.  Returns (o, lse); lse, fp32 [B,Hq,T], only with ``want_lse`` (the
         gradient needs it)."""
         if o is None:
-            o = _like(q)
+            o = _like(q, stream)
         key = ("window", window, sinks, _look(q), _look(k), _look(v), _look(lengths), _look(o), _look(lse))
         e = self._calls.get(key) or self._window(key, "forward", window, sinks, lse, ("lengths", lengths), q=q, k=k, v=v, o=o)
         p = e.p
         p.scale = 1.0 / math.sqrt(p.d) if scale is None else scale
         if lse is None and want_lse:
-            lse = torch.empty((p.B, p.Hq, p.T), dtype=torch.float32, device=q.device)
+            lse = _empty((p.B, p.Hq, p.T), torch.float32, q.device, stream)
         rc = self._lib.lasad_window_attention(self._h, e.ref, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(lengths),
                                               o.data_ptr(), _ptr(lse), _stream(q.device, stream))
         if rc:
@@ -350,9 +348,9 @@ class Mixers:
     def lasad_window_attention_backward(self, q, k, v, o, lse, do, window, sinks=0, scale=None, lengths=None, dq=None,
                                         dk=None, dv=None, workspace=None, stream=None):
         """The gradient of ``lasad_window_attention`` from its inputs and outputs; returns (dq, dk, dv)."""
-        dq = _like(q) if dq is None else dq
-        dk = _like(k) if dk is None else dk
-        dv = _like(v) if dv is None else dv
+        dq = _like(q, stream) if dq is None else dq
+        dk = _like(k, stream) if dk is None else dk
+        dv = _like(v, stream) if dv is None else dv
         key = ("window'", window, sinks, _look(q), _look(k), _look(v), _look(o), _look(lse), _look(do),
                _look(lengths), _look(dq), _look(dk), _look(dv))
         e = self._calls.get(key)
@@ -377,7 +375,7 @@ class Mixers:
         window, Hk, d], which get the token's k and v.  ``pos`` int32 [B]: the tokens' positions
         (negative: the sequence takes no part).  Returns o [B,Hq,d]."""
         if o is None:
-            o = _like(q)
+            o = _like(q, stream)
         key = ("window1", window, sinks, _look(q), _look(k), _look(v), _look(k_cache), _look(v_cache), _look(pos),
                _look(o))
         e = self._calls.get(key)

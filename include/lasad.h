@@ -313,7 +313,7 @@ typedef struct lasad_scan_params {
 /* Bytes of workspace of lasad_scan_forward and lasad_scan_backward, or a negative LASAD_ERR_*. */
 int64_t lasad_scan_workspace(lasad_ctx* ctx, const lasad_scan_params* p);
 /*
- *   x, gate, y   [B,T,C]           h_in, h_out  [B,C] fp32 or NULL
+ *   x, gate, y   [B,T,C]           h_in, h_out  [B,C] fp32 or NULL; h_out may alias h_in
  *   saved        [B, ceil(T / LASAD_SCAN_CHUNK), C] fp32 or NULL: h before every chunk, which the
  *                backward needs
  */
@@ -321,7 +321,7 @@ int lasad_scan_forward(lasad_ctx* ctx, const lasad_scan_params* p, const void* x
                        const float* h_in, void* y, float* h_out, float* saved, void* workspace, void* cuda_stream);
 /*
  * The gradient: dy [B,T,C] and dh_out [B,C] fp32 (or NULL) to dx, dgate [B,T,C] (the gradient of
- * lambda, or of the pre-activation) and dh_in [B,C] fp32 (or NULL).
+ * lambda, or of the pre-activation) and dh_in [B,C] fp32 (or NULL), which may alias dh_out.
  */
 int lasad_scan_backward(lasad_ctx* ctx, const lasad_scan_params* p, const void* x, const void* gate,
                         const float* saved, const void* dy, const float* dh_out, void* dx, void* dgate, float* dh_in,

@@ -217,7 +217,10 @@ struct Work {
         first = segs == 1 ? 0 : seg * a.seg_chunks;
         end = segs == 1 ? chunks : min(first + a.seg_chunks, chunks);
     }
-    // (A, H) or (A, Q) of segment s of this CTA's tile: 2 x width floats
+    // (A, H) or (A, Q) of segment s of this CTA's tile: 2 x width floats.  The last segment of a walk has nothing
+    // behind it and no summary: its place (forward the last one, backward the first) has a copy of the state that the
+    // walk starts from, from which every segment of the second launch starts.  So the state at the walk's end, which
+    // one of them stores, may have the memory of the state at its start.
     __device__ __forceinline__ float* span(const ScanArgs& a, int s) const
     {
         return a.ws + ((long long)s * cuts + cut) * 2 * width;
@@ -350,7 +353,8 @@ __global__ void __launch_bounds__(LC * kSlots, LC == 16 ? 3 : 1) scan_forward_ke
     // the state at the segment's first token: h_in through the segments before it
     N h0 = N::all(0.0f), total = N::all(1.0f);
     if (!SUMMARY && in) {
-        if (a.h_in) h0 = load_state<VEC>(a.h_in + state);
+        if (wk.segs > 1) h0 = load_state<VEC>(wk.span(a, wk.segs - 1) + lane * VEC);
+        else if (a.h_in) h0 = load_state<VEC>(a.h_in + state);
 #pragma unroll 4
         for (int s = 0; s < wk.seg; ++s) {
             const float* w = wk.span(a, s) + lane * VEC;
@@ -436,6 +440,7 @@ __global__ void __launch_bounds__(LC * kSlots, LC == 16 ? 3 : 1) scan_forward_ke
             float* w = wk.span(a, wk.seg) + lane * VEC;
             store_state<VEC>(w, total);
             store_state<VEC>(w + LC * VEC, h0);
+            if (wk.seg == 0) store_state<VEC>(wk.span(a, wk.segs - 1) + lane * VEC, a.h_in ? load_state<VEC>(a.h_in + state) : N::all(0.0f));
         }
     }
 }
@@ -477,7 +482,8 @@ __global__ void __launch_bounds__(LC * kSlots, LC != 16 ? 1 : sizeof(T) == 2 ? 2
     N u0 = N::all(0.0f), total = N::all(1.0f), hs = N::all(0.0f);      // hs: h before the chunk
     if (!SUMMARY && in) {
         hs = load_state<VEC>(saved);
-        if (a.dh_out) u0 = load_state<VEC>(a.dh_out + state);
+        if (wk.segs > 1) u0 = load_state<VEC>(wk.span(a, 0) + lane * VEC);
+        else if (a.dh_out) u0 = load_state<VEC>(a.dh_out + state);
 #pragma unroll 4
         for (int s = wk.segs - 1; s > wk.seg; --s) {
             const float* w = wk.span(a, s) + lane * VEC;
@@ -593,6 +599,7 @@ __global__ void __launch_bounds__(LC * kSlots, LC != 16 ? 1 : sizeof(T) == 2 ? 2
             float* w = wk.span(a, wk.seg) + lane * VEC;
             store_state<VEC>(w, total);
             store_state<VEC>(w + LC * VEC, u0);
+            if (wk.seg == wk.segs - 1) store_state<VEC>(wk.span(a, 0) + lane * VEC, a.dh_out ? load_state<VEC>(a.dh_out + state) : N::all(0.0f));
         }
     }
 }

@@ -171,7 +171,8 @@ class Mixers:
                            h_out=None, want_state=True, save=False, workspace=None, stream=None):
         """Gated linear recurrence with the spatial rule over [B,T,C]; returns (y, h_out, saved).
         ``gate`` holds lambda, or with ``logits`` its pre-activation; ``tied`` scales x by 1 - lambda.
-        ``save`` keeps the states that ``lasad_scan_backward`` needs."""
+        ``save`` keeps the states that ``lasad_scan_backward`` needs.  ``h_out`` may be ``h_in``: a sequence
+        taken in pieces carries its state in place."""
         if y is None:
             y = _like(x, stream)
         key = ("scan", _look(x), _look(gate), _look(h_in), _look(y), _look(h_out))
@@ -190,7 +191,7 @@ class Mixers:
 
     def lasad_scan_backward(self, x, gate, saved, dy, dh_out=None, grid_w=0, prefix_len=0, t0=0, tied=True, logits=False,
                             dx=None, dgate=None, dh_in=None, want_state=True, workspace=None, stream=None):
-        """The gradient of ``lasad_scan_forward``; returns (dx, dgate, dh_in)."""
+        """The gradient of ``lasad_scan_forward``; returns (dx, dgate, dh_in).  ``dh_in`` may be ``dh_out``."""
         if dx is None:
             dx = _like(x, stream)
         if dgate is None:

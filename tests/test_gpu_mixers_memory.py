@@ -62,3 +62,40 @@ def test_weight_gradients_on_two_streams(ctx):
     q, k, dq, dk = (draw(n, 4, 2000, 8, 64, dtype=BF16) for n in (1, 2, 3, 4))
     table, w = binding.rope_table(2000, 64, False, device="cuda"), draw(5, 64)
     check_two_streams(ctx, lambda **s: ctx.lasad_qk_norm_rope_backward(q, k, table, dq, dk, w, w, **s))
+
+
+# ---------------------------------------------------------------------------------------------
+# states written where they were read
+# ---------------------------------------------------------------------------------------------
+PIECES = [  # B, T, C, tokens of the first piece: pieces that are cut into segments (8 chunks of 128 and more) and whole
+    (1, 3000, 64, 1500), (2, 2500, 34, 1100), (3, 2100, 96, 60), (1, 4700, 1536, 2350),
+]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("shape", PIECES)
+def test_recurrence_carries_its_state_in_place(ctx, shape, dtype):
+    """A sequence in two pieces with the state, and its gradient, in one piece of memory: the same bits as with
+    memory of their own for each."""
+    B, T, C, cut = shape
+    x, z, dy = (draw(n, B, T, C, dtype=dtype) for n in (1, 2, 3))
+    h_in, dh_out = draw(4, B, C), draw(5, B, C)
+    kw = dict(grid_w=24, prefix_len=1, logits=True)
+    halves = [(t[:, :cut], t[:, cut:]) for t in (x, z, dy)]
+
+    def run(place):
+        """place(t): where the state that replaces t goes."""
+        h, u, ys, saves, grads = h_in.clone(), dh_out.clone(), [], [], []
+        for n, t0 in ((0, 0), (1, cut)):
+            y, h, saved = ctx.lasad_scan_forward(halves[0][n], halves[1][n], t0=t0, h_in=h, h_out=place(h), save=True, **kw)
+            ys.append(y)
+            saves.append(saved)
+        for n, t0 in ((1, cut), (0, 0)):
+            dx, dz, u = ctx.lasad_scan_backward(halves[0][n], halves[1][n], saves[n], halves[2][n], t0=t0, dh_out=u,
+                                                dh_in=place(u), **kw)
+            grads += [dx, dz]
+        return ys + saves + grads + [h, u]
+    apart = run(lambda t: None)
+    for _ in range(5):
+        for a, b in zip(run(lambda t: t), apart):
+            assert torch.equal(a, b)

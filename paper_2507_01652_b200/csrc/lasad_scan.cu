@@ -119,9 +119,10 @@ __device__ __forceinline__ void store_state(float* p, num<VEC> x)
     for (int v = 0; v < VEC; ++v) p[v] = x.get(v);
 }
 
-// lambda = sigmoid(z) = 1 / (1 + t) and 1 - lambda = t / (1 + t) with t = e^-z, each to full
-// relative precision.  The exponent ends at 126, where lambda is 2^-126 and the products stay finite;
-// a NaN passes through.
+// lambda = sigmoid(z) = 1 / (1 + t) and 1 - lambda = t / (1 + t) with t = e^-z, neither as a difference: both
+// have the relative error of t, about (|z| + 4) 2^-23 (the exponent's rounding and that of the hardware's power
+// and reciprocal), however small they are.  The exponent ends at 126, where lambda is 2^-126 and the products
+// stay finite; a NaN passes through.
 template <bool LOGITS, int VEC>
 __device__ __forceinline__ void gate_of(num<VEC> z, num<VEC>& lam, num<VEC>& rest)
 {
@@ -563,10 +564,14 @@ __global__ void __launch_bounds__(LC * kSlots, LC != 16 ? 1 : sizeof(T) == 2 ? 2
                 N f = TIED ? fma(xv[t], minus, prev) : prev;
                 if (LOGITS) f = f * (rest[t] * ca[t]);             // the derivative of the sigmoid
                 if (ends && ((ends >> t) & 1u)) {
-                    // a row's last token does not pass h on through lambda; ca is 1 there, and lambda
-                    // is formed again (2^-24 off at most, as the term it scales is)
+                    // a row's last token does not pass h on through lambda; ca is 1 there, and lambda is formed
+                    // again from the gate (not as 1 - rest, which has lost it where lambda is small)
                     f = TIED ? xv[t] * minus : N::all(0.0f);
-                    if (LOGITS) f = f * (rest[t] * fma(rest[t], minus, N::all(1.0f)));
+                    if (LOGITS) {
+                        N lam, same;
+                        gate_of<true>(P::get(st.get(buf, 0, t)), lam, same);
+                        f = f * (rest[t] * lam);
+                    }
                 }
                 xv[t] = f;
             }

@@ -1,0 +1,52 @@
+"""Edges of the operators beside LASAD: gates that are nearly shut, grids and positions near the ends of their types,
+calls that have to be refused."""
+import pytest
+import torch
+
+from paper_2507_01652_b200 import binding
+from tests import _mixers_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    torch.cuda.set_device(0)
+    c = binding.Lasad(0)
+    yield c
+    c.close()
+
+
+def draw(seed, *shape, dtype=F32):
+    return torch.randn(*shape, generator=torch.Generator().manual_seed(seed)).to(dtype)
+
+
+@pytest.mark.parametrize("C", [64, 33])
+@pytest.mark.parametrize("tied", [True, False])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_gate_gradient_at_row_ends_of_nearly_shut_gates(ctx, dtype, tied, C):
+    """Logits from -15 to -60 (lambda from 3e-7 to 1e-26).  On a row's last token the tied gate's gradient is
+    -g x lambda (1 - lambda), as small as lambda, and 0 untied.  Each value on its own: lambda carries (|z| + 4) 2^-23
+    (2^-17), the products and g, which is dy and a share of lambda from the right, a few 2^-24; a bf16 gradient
+    its rounding of 2^-8."""
+    B, T, w = 2, 200, 5
+    x, dy = draw(1, B, T, C, dtype=dtype), draw(2, B, T, C, dtype=dtype)
+    z = -15 - 45 * torch.rand(B, T, C, generator=torch.Generator().manual_seed(3))
+    z = z.to(dtype)
+    leaves = [t.double().requires_grad_() for t in (x, z)]
+    y, _ = ref.scan(*leaves, None, w, 0, 0, tied, True)
+    # (autograd forms the derivative of sigmoid(-z) as s (1 - s), which is 0 in 64 bits too from z = -37 on: the
+    # formula instead, with g = dx / (1 - lambda) where tied)
+    dx, dz = torch.autograd.grad(y, leaves, dy.double())
+    z64 = z.double()
+    want = -dx * x.double() * torch.sigmoid(z64) if tied else dz
+    _, _, saved = ctx.lasad_scan_forward(x.cuda(), z.cuda(), grid_w=w, tied=tied, logits=True, save=True)
+    _, got, _ = ctx.lasad_scan_backward(x.cuda(), z.cuda(), saved, dy.cuda(), grid_w=w, tied=tied, logits=True)
+    ends = [t for t in range(T) if ref.ends_row(t, w, 0)]
+    got, want = got.cpu().double()[:, ends], want[:, ends]
+    if not tied:
+        assert bool((got == 0).all()) and bool((want == 0).all())
+        return
+    assert bool(((got - want).abs() <= (2.0 ** -16 + (2.0 ** -8 if dtype == BF16 else 0)) * want.abs()).all())

@@ -167,7 +167,7 @@ struct RowEnds {
         if (w <= 0) return 0u;
         unsigned m = 0;
         const long long first = j >= 0 ? w - 1 - col : w - 1 - j;
-        for (int e = first < kTok ? (int)first : kTok; e < kTok; e += w) m |= 1u << e;
+        for (int e = first < kTok ? (int)first : kTok; e < kTok; e += min(w, kTok)) m |= 1u << e;
         return m;
     }
     __device__ __forceinline__ void forward()
@@ -176,8 +176,7 @@ struct RowEnds {
         j += by;
         if (w <= 0) return;
         if (on) {
-            col += step;
-            if (col >= w) col -= w;
+            col = col < w - step ? col + step : col - (w - step);      // (a sum may pass 2^31)
         } else if (j >= 0) {
             col = (int)(j % w);
         }

@@ -50,3 +50,31 @@ def test_gate_gradient_at_row_ends_of_nearly_shut_gates(ctx, dtype, tied, C):
         assert bool((got == 0).all()) and bool((want == 0).all())
         return
     assert bool(((got - want).abs() <= (2.0 ** -16 + (2.0 ** -8 if dtype == BF16 else 0)) * want.abs()).all())
+
+
+@pytest.mark.parametrize("C", [64, 33])
+@pytest.mark.parametrize("w", [2 ** 30 + 50, 2 ** 31 - 60, 2 ** 31 - 1])
+def test_recurrence_on_rows_near_2_to_31_tokens(ctx, w, C):
+    """A walk over the end of a grid row whose width, and the tokens' columns on it, fill an int32: the row's last
+    token lets h through whole, the ones 128 and 256 further on do not."""
+    T, P = 400, 3
+    t0 = P + w - 1 - 130                       # the row ends at token 130 of the call
+    x, gate, dy = draw(1, 1, T, C), torch.sigmoid(draw(2, 1, T, C)), draw(3, 1, T, C)
+    leaves = [t.double().requires_grad_() for t in (x, gate)]
+    y, _ = ref.scan(*leaves, None, w, P, t0, True, False)
+    assert [t for t in range(T) if ref.ends_row(t0 + t, w, P)] == [130]
+    want = torch.autograd.grad(y, leaves, dy.double())
+    kw = dict(grid_w=w, prefix_len=P, t0=t0)
+    got, _, saved = ctx.lasad_scan_forward(x.cuda(), gate.cuda(), save=True, **kw)
+    back = ctx.lasad_scan_backward(x.cuda(), gate.cuda(), saved, dy.cuda(), **kw)
+    for a, b in zip((got,) + back[:2], (y.detach(),) + want):
+        # fp32: 2^-22 of each value and 2^-20 of the largest (sums of some tens of terms)
+        assert bool(((a.cpu().double() - b).abs() <= 2.0 ** -22 * b.abs() + 2.0 ** -20 * b.abs().max()).all())
+    state = torch.zeros(1, C, device="cuda")
+    for t in range(128, 133):
+        pos = None if t0 + t > 2 ** 31 - 1 else torch.tensor([t0 + t], dtype=torch.int32, device="cuda")
+        before = state.clone()
+        step, _ = ctx.lasad_scan_step(x[:, t].cuda(), gate[:, t].cuda(), state, t=t0 + t, grid_w=w, prefix_len=P, pos=pos)
+        lam = torch.ones_like(gate[:, t]) if t == 130 else gate[:, t]
+        want_h = lam.double() * before.cpu().double() + (1 - gate[:, t].double()) * x[:, t].double()
+        assert bool(((step.cpu().double() - want_h).abs() <= 2.0 ** -21).all())

@@ -281,7 +281,7 @@ int lasad_decode_step_fused(lasad_ctx* ctx, const lasad_params* p,
  * the caller's `workspace` (16-byte aligned device memory of the size that the matching query
  * returns; NULL where that is 0), which is free again once the stream has passed the call.  They
  * allocate nothing, may be recorded into a CUDA graph, and give the same bits on every run.
- * B <= 65535; f32 tensors may not be mixed with bf16 ones in one call.
+ * B <= 65535; 0 <= t0 <= 2^62; f32 tensors may not be mixed with bf16 ones in one call.
  * ---------------------------------------------------------------------------------------------- */
 
 /*

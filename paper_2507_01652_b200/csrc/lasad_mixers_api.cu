@@ -38,6 +38,8 @@ bool strides_ok(const int64_t* s, int64_t esz, int B, int T, int H, int d)
         if (s[i] < 0 || (s[i] * esz) % 16 != 0) return false;
     return (s[0] > 0 || B == 1) && (s[1] > 0 || T == 1) && (s[2] >= d || H == 1);
 }
+// A first position that leaves room for T tokens, and for the chunk behind the last one, in 64 bits.
+bool first_ok(int64_t t0) { return t0 >= 0 && t0 <= (int64_t)1 << 62; }
 void copy3(long long (&to)[3], const int64_t* from)
 {
     for (int i = 0; i < 3; ++i) to[i] = from[i];
@@ -47,8 +49,8 @@ void copy3(long long (&to)[3], const int64_t* from)
 int scan_args(lasad_ctx* ctx, const lasad_scan_params* p, bool step, bool backward, lasad::ScanArgs& a)
 {
     if (!ctx || !p) return LASAD_ERR_INVALID_ARG;
-    if (p->B <= 0 || p->C <= 0 || (!step && p->T <= 0) || p->grid_w < 0 || p->prefix_len < 0 || p->t0 < 0 ||
-        p->reserved != 0 || (p->flags & ~(LASAD_SCAN_TIED | LASAD_SCAN_LOGITS)) ||
+    if (p->B <= 0 || p->C <= 0 || (!step && p->T <= 0) || p->grid_w < 0 || p->prefix_len < 0 ||
+        !first_ok(p->t0) || p->reserved != 0 || (p->flags & ~(LASAD_SCAN_TIED | LASAD_SCAN_LOGITS)) ||
         (p->dtype != LASAD_F32 && p->dtype != LASAD_BF16))
         return LASAD_ERR_INVALID_ARG;
     const int64_t* strides[] = {p->x_stride, p->gate_stride, p->y_stride, p->dx_stride, p->dgate_stride};
@@ -84,7 +86,7 @@ int rope_args(lasad_ctx* ctx, const lasad_rope_params* p, bool backward, bool ha
 {
     if (!ctx || !p) return LASAD_ERR_INVALID_ARG;
     if (p->B <= 0 || p->T <= 0 || p->Hq <= 0 || p->Hk <= 0 || p->d <= 0 || p->grid_w < 0 || p->prefix_len < 0 ||
-        p->t0 < 0 || p->table_rows <= 0 || p->reserved != 0 || (p->flags & ~LASAD_ROPE_HALF) || !(p->eps >= 0.0f) ||
+        !first_ok(p->t0) || p->table_rows <= 0 || p->reserved != 0 || (p->flags & ~LASAD_ROPE_HALF) || !(p->eps >= 0.0f) ||
         !std::isfinite(p->eps) || (p->dtype != LASAD_F32 && p->dtype != LASAD_BF16))
         return LASAD_ERR_INVALID_ARG;
     const int64_t* strides[2][4] = {{p->q_stride, p->q_out_stride, p->dq_out_stride, p->dq_stride},

@@ -78,3 +78,24 @@ def test_recurrence_on_rows_near_2_to_31_tokens(ctx, w, C):
         lam = torch.ones_like(gate[:, t]) if t == 130 else gate[:, t]
         want_h = lam.double() * before.cpu().double() + (1 - gate[:, t].double()) * x[:, t].double()
         assert bool(((step.cpu().double() - want_h).abs() <= 2.0 ** -21).all())
+
+
+def refused(fn, *a, **kw):
+    with pytest.raises(binding.LasadError) as e:
+        fn(*a, **kw)
+    return e.value.code == binding.LASAD_ERR_INVALID_ARG
+
+
+def test_positions_that_are_no_numbers_are_refused(ctx):
+    """t0 past 2^62: a sum that wraps round at 2^63 would look like a position before the table's end."""
+    x, q = torch.zeros(1, 4, 32, device="cuda"), torch.zeros(1, 4, 2, 64, device="cuda")
+    table, grid = (binding.rope_table(16, 64, g, device="cuda") for g in (False, True))
+    for t0 in (2 ** 63 - 1, 2 ** 63 - 4, 2 ** 62 + 1):
+        assert refused(ctx.lasad_scan_forward, x, x, t0=t0)
+        assert refused(ctx.lasad_scan_backward, x, x, torch.zeros(1, 1, 32, device="cuda"), x, t0=t0)
+        assert refused(ctx.lasad_qk_norm_rope, q, q, table, t0=t0)
+        assert refused(ctx.lasad_qk_norm_rope, q, q, grid, grid_w=8, t0=t0)
+        assert refused(ctx.lasad_qk_norm_rope_backward, q, q, table, q, q, t0=t0)
+    assert refused(ctx.lasad_scan_step, x[:, 0], x[:, 0], torch.zeros(1, 32, device="cuda"), t=2 ** 63 - 1)
+    y, _, _ = ctx.lasad_scan_forward(x, x, t0=2 ** 62, grid_w=7)        # the largest ones are positions
+    assert bool((y == 0).all())

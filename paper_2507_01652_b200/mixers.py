@@ -73,12 +73,12 @@ def rope_table(rows: int, d: int, grid: bool, base: float = 10000.0, device=None
     return torch.stack((a.cos(), a.sin()), dim=-1).to(torch.float32).to(device)
 
 
-# What a call looks like: the shape, strides, type and place of every tensor, or None.  A call that
+# What a call looks like: the shape, strides, type and device of every tensor, or None.  A call that
 # looks like one before it has been checked and has its params struct and workspace size already
 # (checking and building them costs more than the rest of the call); scalars are set again each time.
 # A context keeps its own (``_calls``): like the context, they serve one host thread at a time.
 def _look(t):
-    return None if t is None else (t.shape, t.stride(), t.dtype, t.is_cuda)
+    return None if t is None else (t.shape, t.stride(), t.dtype, t.get_device())
 
 
 def _like(t, stream):
@@ -126,6 +126,13 @@ def _strides2(t):
 class Mixers:
     """The calls beside LASAD; a base of ``binding.Lasad``, which has the library and the context."""
 
+    def _here(self, *ts):
+        """The tensors that are there are on the context's device."""
+        _check_cuda(*ts)
+        for t in ts:
+            if t is not None and t.get_device() != self.device:
+                raise ValueError(f"all tensors must be on cuda:{self.device}, the context's device, not on {t.device}")
+
     def _new(self, key, p):
         if len(self._calls) > 256:
             self._calls.clear()
@@ -139,8 +146,8 @@ class Mixers:
                 self._raise(int(n), query.__name__)
             e.ws = int(n)
         if given is not None:
-            if not given.is_cuda or not given.is_contiguous() or given.numel() * given.element_size() < e.ws:
-                raise ValueError(f"workspace must be contiguous CUDA memory of at least {e.ws} bytes")
+            if given.get_device() != self.device or not given.is_contiguous() or given.numel() * given.element_size() < e.ws:
+                raise ValueError(f"workspace must be contiguous memory of cuda:{self.device} of at least {e.ws} bytes")
             return given
         if not e.ws:
             return None
@@ -149,7 +156,7 @@ class Mixers:
     # ---- gated linear recurrence ------------------------------------------------------------
     def _scan(self, key, kind, x, gate, y, dx, dgate, states, saved, pos):
         """Checks a call that looks like none before it.  states: (name, tensor) of [B,C]."""
-        _check_cuda(x, gate, y, dx, dgate, saved, pos, *(t for _, t in states))
+        self._here(x, gate, y, dx, dgate, saved, pos, *(t for _, t in states))
         _same("x, gate and their outputs and gradients", x, gate, y, dx, dgate)
         if x.dim() != (2 if kind == "step" else 3):
             raise ValueError("expected [B,C]" if kind == "step" else "expected [B,T,C]")
@@ -236,7 +243,7 @@ class Mixers:
     def _rope(self, key, q, k, table, q_weight, k_weight, pos, grid, outs):
         """Checks a call that looks like none before it.  outs: the (up to six) tensors after q and k
         in the order of the params' strides, or None."""
-        _check_cuda(q, k, table, q_weight, k_weight, pos, *outs)
+        self._here(q, k, table, q_weight, k_weight, pos, *outs)
         _same("q, k and their outputs and gradients", q, k, *outs)
         if q.dim() != 4 or k.dim() != 4:
             raise ValueError("expected [B,T,H,d]")
@@ -306,7 +313,7 @@ class Mixers:
     def _window(self, key, kind, window, sinks, lse, ints, **ts):
         """Checks a call that looks like none before it.  ints: (name, tensor) of int32 [B]; the other
         tensors by name: those of a step have no token dimension, caches always have slots."""
-        _check_cuda(lse, ints[1], *ts.values())
+        self._here(lse, ints[1], *ts.values())
         first = ts["q"] if "q" in ts else ts["k"]
         _same("all tensors", first, *ts.values())
         k = ts["k"]

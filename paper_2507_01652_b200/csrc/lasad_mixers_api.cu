@@ -101,8 +101,9 @@ int rope_args(lasad_ctx* ctx, const lasad_rope_params* p, bool backward, bool ha
     if (!has_pos) {     // the largest index into the table
         int64_t last = p->t0 + p->T - 1;
         if (p->grid_w > 0) {
-            const int64_t j = last - p->prefix_len;
-            last = j < 0 ? 0 : j >= p->grid_w - 1 ? std::max<int64_t>(j / p->grid_w, p->grid_w - 1) : j;
+            const int64_t w = p->grid_w, first = std::max<int64_t>(p->t0 - p->prefix_len, 0), j = last - p->prefix_len;
+            // (tokens of one grid row: its number or the last one's column; of several: a row's last column is among theirs)
+            last = j < 0 ? 0 : std::max(j / w, first / w == j / w ? j % w : w - 1);
         }
         if (last >= p->table_rows) return LASAD_ERR_INVALID_ARG;
     }

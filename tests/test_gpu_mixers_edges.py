@@ -99,3 +99,28 @@ def test_positions_that_are_no_numbers_are_refused(ctx):
     assert refused(ctx.lasad_scan_step, x[:, 0], x[:, 0], torch.zeros(1, 32, device="cuda"), t=2 ** 63 - 1)
     y, _, _ = ctx.lasad_scan_forward(x, x, t0=2 ** 62, grid_w=7)        # the largest ones are positions
     assert bool((y == 0).all())
+
+
+@pytest.mark.parametrize("t0,T,fits", [
+    (1 + 96 * 5 + 2, 3, True),          # row 5, columns 2 to 4
+    (1 + 96 * 5 + 2, 6, True),          # ... to column 7, the table's last row
+    (1 + 96 * 5 + 2, 7, False),         # ... to column 8
+    (1 + 96 * 7, 1, True), (1 + 96 * 8, 1, False),
+    (1 + 96 * 4 + 94, 4, False),        # over the end of a row: column 95
+    (0, 9, True), (0, 10, False), (0, 1, True),
+])
+def test_rotation_takes_every_position_that_its_table_has(ctx, t0, T, fits):
+    """A table of 8 rows for a grid of 96 columns and one token before it: a call is refused where a token's row or
+    column is not in the table, and only there."""
+    q = draw(1, 1, T, 2, 64).cuda()
+    table = binding.rope_table(8, 64, True, device="cuda")
+    kw = dict(grid_w=96, prefix_len=1, t0=t0)
+    if not fits:
+        assert refused(ctx.lasad_qk_norm_rope, q, q, table, **kw)
+        assert refused(ctx.lasad_qk_norm_rope_backward, q, q, table, q, q, **kw)
+        return
+    y, _ = ctx.lasad_qk_norm_rope(q, q, table, **kw)
+    ctx.lasad_qk_norm_rope_backward(q, q, table, q, q, **kw)
+    want = ref.rope_one(q.cpu().double(), None, t0, 96, 1, False, 1e-6)
+    # fp32: 2^-22 of each value and 2^-20 of the largest
+    assert bool(((y.cpu().double() - want).abs() <= 2.0 ** -22 * want.abs() + 2.0 ** -20 * want.abs().max()).all())

@@ -382,7 +382,7 @@ int lasad_qk_norm_rope_backward(lasad_ctx* ctx, const lasad_rope_params* p, cons
  *     o_t = sum_{s in V(t)} p_ts v_s ,   p_ts = e^(scale q_t.k_s) / sum_{V(t)} e^(scale q_t.k_s) .
  *
  *   q, o [B,T,Hq,d], k, v [B,T,Hk,d], d in {32, 64}, Hk divides Hq (query head h reads key head
- *   h / (Hq / Hk)), 1 <= window, 0 <= sinks <= 128.
+ *   h / (Hq / Hk)), 1 <= window (with a cache <= 2^30), 0 <= sinks <= 128.
  *   lengths [B] int32 (device) or NULL: sequence b ends before token lengths[b] (0 to T).  A row
  *   past the end is empty: its o and gradients are 0 and its lse is -infinity, and nothing that
  *   stands in q, k, v, o, do there counts, not even a NaN.  (A NaN or an infinity before the end may

@@ -148,7 +148,8 @@ int window_args(lasad_ctx* ctx, const lasad_window_params* p, int what, lasad::W
         if (!strides_ok(s, esz, p->B, t.n, t.H, p->d)) return LASAD_ERR_INVALID_ARG;
         for (int i = 0; i < 3; ++i) t.to[i] = s[i];
     }
-    if ((p->d != 32 && p->d != 64) || p->sinks > lasad::kMaxSinks || p->B > 65535 || p->window > (1 << 30))
+    if ((p->d != 32 && p->d != 64) || p->sinks > lasad::kMaxSinks || p->B > 65535 ||
+        ((what == kStep || what == kStore) && p->window > (1 << 30)))
         return LASAD_ERR_UNSUPPORTED;
     if ((int64_t)p->B * p->Hq * ((T + 31) / 32) > 0x7fffffffLL || T > (1 << 30) || p->Hk > 65535)
         return LASAD_ERR_UNSUPPORTED;

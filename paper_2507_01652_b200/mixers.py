@@ -331,7 +331,8 @@ class Mixers:
         _i32(ints[0], ints[1], B)
         _f32("lse", lse, (B, Hq, T))
         st = [(_I64 * 3)() if n not in ts else (_strides3 if ts[n].dim() == 4 else _strides_decode)(ts[n]) for n in self._ORDER]
-        return self._new(key, WindowParams(B, T, Hq, Hk, d, _dtype_code(first), window, sinks, 0.0, 0, *st))
+        # (a struct's int32 would take a longer window's lowest bits; no sequence is longer than the longest of them)
+        return self._new(key, WindowParams(B, T, Hq, Hk, d, _dtype_code(first), min(window, 2 ** 31 - 1), sinks, 0.0, 0, *st))
 
     def lasad_window_attention(self, q, k, v, window, sinks=0, scale=None, lengths=None, o=None, lse=None,
                                want_lse=False, stream=None):

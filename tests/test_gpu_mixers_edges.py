@@ -124,3 +124,16 @@ def test_rotation_takes_every_position_that_its_table_has(ctx, t0, T, fits):
     want = ref.rope_one(q.cpu().double(), None, t0, 96, 1, False, 1e-6)
     # fp32: 2^-22 of each value and 2^-20 of the largest
     assert bool(((y.cpu().double() - want).abs() <= 2.0 ** -22 * want.abs() + 2.0 ** -20 * want.abs().max()).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_windows_longer_than_any_sequence(ctx, dtype):
+    """They hide nothing, whatever their size: the same bits as a window of the sequence's length."""
+    q, k, v, do = (draw(n, 2, 150, h, 64, dtype=dtype).cuda() for n, h in ((1, 4), (2, 2), (3, 2), (4, 4)))
+
+    def run(window):
+        o, lse = ctx.lasad_window_attention(q, k, v, window, 1, want_lse=True)
+        return (o, lse) + ctx.lasad_window_attention_backward(q, k, v, o, lse, do, window, 1)
+    want = run(150)
+    for window in (151, 2 ** 30 + 1, 2 ** 31 - 1, 2 ** 32 + 3, 2 ** 63 - 1):
+        assert all(torch.equal(a, b) for a, b in zip(run(window), want)), window

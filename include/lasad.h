@@ -327,7 +327,8 @@ int lasad_scan_backward(lasad_ctx* ctx, const lasad_scan_params* p, const void* 
                         const float* saved, const void* dy, const float* dh_out, void* dx, void* dgate, float* dh_in,
                         void* workspace, void* cuda_stream);
 /* One token: x, gate, y [B,C]; h_in, h_out [B,C] fp32 (may be the same memory).  pos [B] int32
- * (device): each sequence's absolute position, or NULL for t0. */
+ * (device): each sequence's absolute position, or NULL for t0.  (As in lasad_decode_step_pos, a negative one is
+ * a position before the grid: the state moves on.  lasad_window_attention_step leaves such a sequence out.) */
 int lasad_scan_step(lasad_ctx* ctx, const lasad_scan_params* p, const void* x, const void* gate, const float* h_in,
                     void* y, float* h_out, const int32_t* pos, void* cuda_stream);
 
@@ -390,7 +391,8 @@ int lasad_qk_norm_rope_backward(lasad_ctx* ctx, const lasad_rope_params* p, cons
  *   lse [B,Hq,T] fp32: log of the row's sum of e^(scale q.k); may be NULL in the forward.
  * With bf16 the products run on the tensor cores with fp32 accumulation, statistics and exponentials
  * in fp32; the weights p and the gradients of the scores are rounded to bf16 where they enter a
- * product.  With f32 everything is fp32.
+ * product (results are then off by 0.21 to 0.24 % of their size, of which bf16's own rounding is 0.17;
+ * LASAD_OPT_WINDOW_IMPL = 1 keeps both in fp32, on the CUDA cores).  With f32 everything is fp32.
  */
 typedef struct lasad_window_params {
     int32_t B, T, Hq, Hk, d; /* T: tokens (ignored by the step) */

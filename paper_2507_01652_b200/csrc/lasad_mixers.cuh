@@ -27,8 +27,8 @@ inline cudaError_t launch_dependent(void (*kernel)(P...), dim3 grid, dim3 block,
 
 #ifdef __CUDACC__
 // (It does not let the next launch in early: its CTAs would spread over the SMs as places fall free, and take
-// turns with the ones that still run.  Gradient of the norm and rotation with its forward, 8 x 4096 x 24: 183 us, let
-// in early 191; one recurrence step 2.0 against 2.6.)
+// turns with the ones that still run.  Launches one after another in a graph: gradient of the norm and rotation with its
+// forward, 8 x 4096 x 24, 184 us, let in early 193; one recurrence step 2.1 against 2.6.)
 __device__ __forceinline__ void pdl_wait()
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");

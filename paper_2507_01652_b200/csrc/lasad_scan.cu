@@ -12,8 +12,11 @@
 // neighbouring channels in registers, the slots' pairs meet in shared memory once per chunk, and
 // each thread runs its 8 tokens again from the state that the slots before it leave.  The gradient
 // needs h_{t-1}: the forward keeps h before each chunk in 32 bits (4 bytes per 128 tokens) and the
-// backward forms the rest again from x and lambda, which it reads anyway.  Both passes are bound
-// by device memory: x, lambda and y, and x, lambda, dy, dx and dlambda, each move once.
+// backward forms the rest again from x and lambda, which it reads anyway.  What neither pass can do without
+// is the memory: x, lambda and y, and x, lambda, dy, dx and dlambda, each moved once.  What bounds them now is
+// the instructions around each element and the latency between them at 12 to 24 warps an SM: 8 x 9216 x 1536
+// in bf16, forward 145 us and gradient 283 (1 x 9217 x 1536: 35 and 53), has device memory at half of its rate
+// and 62 to 66 % of the issue slots in use; the exponentials and shared memory are below 40 % of theirs.
 //
 // A CTA walks one tile of channels of one sequence.  Where that gives too few CTAs the sequence is
 // cut into segments: a first launch forms each segment's (A, H) (of the backward: the same pair of
@@ -313,8 +316,9 @@ struct Stage {
 
 // The wait for the launch before.  The next launch is let in early only by a summary whose launch behind it
 // has no whole tiles: CTAs that come while others still run spread over the SMs as places fall free, and the
-// whole walk then goes at the pace of the fullest SM (4 x 2304 x 1536 forward after itself 34 against 29 us, 10
-// x 2304 x 1536, cut in its last round, 61 against 47).
+// whole walk then goes at the pace of the fullest SM (one after another in a graph: 4 x 2304 x 1536 forward 35 against
+// 30 us, 10 x 2304 x 1536, cut in its last round, 63 against 48; the summaries' own early release: forward and gradient
+// of 1 x 9217 x 1536 87.3 against 88.1).
 template <bool SUMMARY> __device__ __forceinline__ void wait_for(const ScanArgs& a)
 {
     if (SUMMARY && a.whole == 0) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -701,14 +705,23 @@ cudaError_t launch(const ScanArgs& a, cudaStream_t st)
 
 // How a call's work is cut.  A tile is 32 channels of one sequence, `slots` the CTAs that run at a time.
 // A segment's summary reads two streams once more, of the forward's three and the backward's five, in a
-// launch before, so a cut has to bring three CTAs in the place of one (backward: two).
-//   - So few tiles, and eight chunks or more: all are cut, into as many segments as there are slots for.  Cut
-//     against whole, us, bf16, forward and gradient: 1 x 9217 x 1536 33 and 51 against 89 and 138, 1 x 1024 x 1536 7.5
-//     and 12.1 against 11.1 and 16.5.  Two segments: 4 x 2304 x 1536 forward 37 against 34, 3 x 2304 x 1536 gradient 39
-//     against 48.  Four chunks (1 x 512 x 1536): 6.5 and 7.8 against 6.2 and 8.9.
+// launch before, so a cut has to bring three CTAs in the place of one (backward: two).  (us below: launches one after
+// another in a graph, bf16 unless said, cut against whole.)
+//   - So few tiles, and eight chunks or more: all are cut, into as many segments as there are slots for.
+//     Forward and gradient: 1 x 9217 x 1536 35.5 and 53 against 89 and 146, 1 x 1024 x 1536 7.4 and 11.5 against 11.1 and
+//     18.1.  Two segments: 4 x 2304 x 1536 forward 31.6 against 30.4, 3 x 2304 x 1536 gradient 36.6 against 38.7.  Four
+//     chunks (1 x 512 x 1536): 6.1 and 7.2 against 6.3 and 9.8 (left whole: one launch).
 //   - A last round of tiles that leaves a quarter of the SMs or more idle: that round is cut.  Gradient of 8 x
-//     2304 x 1536 (88 of 384 tiles) 75 against 82 us, forward in fp32 60 against 67; gradient of 4 x 2304 x 1536 in fp32
-//     (44 of 192) 61 against 80; with 132 of 576 left (12 x 2304 x 1536, forward) 63 against 57.
+//     2304 x 1536 (88 of 384 tiles) 78 against 85, of 4 x 2304 x 1536 in fp32 (44 of 192) 65 against 83; forward of
+//     10 x 2304 x 1536 (36 of 480) 48 against 57, of 8 x 2304 x 1536 in fp32 61 against 67; with 132 of 576 left (12 x
+//     2304 x 1536, forward) 61 against 58.
+//   - After four whole rounds one round more is a fifth of the time at most: no cut.  Forward 38, 47, 57 x 1152 x 1536
+//     82.7, 100.6, 120.4 against 83.6, 101.1, 119.7; what it leaves is the gradient's, 25 and 32 x 1152 x 1536 110 and
+//     140 against 118 and 143, in fp32 13 and 16 x 1152 x 1536 101 and 121 against 108 and 129.
+// The rule counts the slots of the 16-byte kernel for the single-channel one as well, which has twice the threads and one
+// CTA an SM: how much workspace a call needs is asked before its pointers' alignment is known.  Cut against whole
+// there: 1 x 9217 x 1535 forward 100 against 163, gradient 133 against 240, 10 x 2304 x 1535 forward 156 against 169; where
+// its fewer slots make the cut a second round, 3 x 2304 x 1535, 62 against 46 and 82 against 66.
 void scan_plan(ScanArgs& a, bool backward, int sms)
 {
     const long long tiles = (long long)a.B * ((a.C + 31) / 32);

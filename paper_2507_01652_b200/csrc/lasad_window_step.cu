@@ -10,9 +10,9 @@
 // while it is in registers.  Every group of lanes keeps its own running maximum and sum over its
 // rows; they are joined once, by shuffles, and, where several warps have a (sequence, key head), in
 // shared memory.  Who has one goes by how many there are: with 16 and more per SM a warp each (nothing
-// is shared, and a CTA's warps are independent: 256 sequences x 20 heads, 55 MB of keys and values, 16.4 us;
+// is shared, and a CTA's warps are independent: 256 sequences x 20 heads, 55 MB of keys and values, 16.3 us;
 // with a CTA each 27 us); with fewer a CTA of eight warps each, and with fewer than SMs a cluster of up to
-// eight CTAs, whose parts the first one joins (2 x 24 heads of 8 key heads, 4097 slots: 14.4 us; parts in memory and
+// eight CTAs, whose parts the first one joins (2 x 24 heads of 8 key heads, 4097 slots: 14.6 us; parts in memory and
 // a second launch that joins them: 17 us).
 #include "lasad_mixers.cuh"
 #include "lasad_tc_ptx.cuh"

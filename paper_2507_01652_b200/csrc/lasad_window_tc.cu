@@ -17,9 +17,15 @@
 // them latency (S out of TMEM, the maximum, P into TMEM, the barriers), so that three groups bring
 // one every 900.  S, P and O have columns of their own (160 a group, 480 of the SM's 512): the next
 // tile's S is made while this tile's exponentials run.  Measured: 1 x 9217 tokens, 24 query and 8 key
-// heads, window 1536: 168 us; 64 x 577 tokens, 16 heads, window 144: 137 us.  (Two CTAs of two groups
-// with P over S, so that a tile's products stood between two tiles' exponentials: 170 and 162 us; tiles of
-// 128 keys do not fit the registers: 363 us for the first.)
+// heads, window 1536: 162 us; 64 x 577 tokens, 16 heads, window 144: 124 us (in a graph; alone in a cold
+// cache 179 and 136).  (Two CTAs of two groups with P over S, so that a tile's products stood between two
+// tiles' exponentials, cost 170 and 162 us where the step to this form brought 168 and 147; tiles of 128 keys do
+// not fit the registers: 363 us for the first.)
+//
+// P is rounded to bf16 where it enters P V, as the tensor cores take it beside bf16 values: 2^-9 of each term,
+// which adds up like noise (l sums the P that were not rounded).  Against 64 bits o is off by 0.21 % of its size,
+// 0.16 of which is its own rounding to bf16.  P as a sum of two bf16 numbers would cost a second P V and 32 columns
+// a group more than TMEM has; a caller who needs 32 bits has the CUDA-core kernel (LASAD_OPT_WINDOW_IMPL).
 //
 // All waits are bounded (see mbar_wait); a wait that gives up sets the status word and the CTA leaves
 // through the normal exit with its copies landed and its TMEM freed.

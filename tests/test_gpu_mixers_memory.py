@@ -64,6 +64,27 @@ def test_weight_gradients_on_two_streams(ctx):
     check_two_streams(ctx, lambda **s: ctx.lasad_qk_norm_rope_backward(q, k, table, dq, dk, w, w, **s))
 
 
+def test_streams_by_their_handles(ctx):
+    """The default stream by its handle 0, a stream that is current, one that is being captured."""
+    import ctypes
+    x, z = draw(1, 1, 3000, 64), draw(2, 1, 3000, 64)
+    want = ctx.lasad_scan_forward(x, z, logits=True)[:2]
+    torch.cuda.synchronize()
+    for handle in (0, ctypes.c_void_p(0), torch.cuda.current_stream().cuda_stream):
+        got = ctx.lasad_scan_forward(x, z, logits=True, stream=handle)[:2]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = ctx.lasad_scan_forward(x, z, logits=True, stream=torch.cuda.current_stream().cuda_stream)[:2]
+    for t in held:
+        t.fill_(float("nan"))
+    torch.empty(1 << 22, device="cuda").fill_(float("nan"))
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(held, want))
+
+
 # ---------------------------------------------------------------------------------------------
 # states written where they were read
 # ---------------------------------------------------------------------------------------------

@@ -250,10 +250,11 @@ def _plain_packed(s, c):
     if T == 0:
         return out
     at = _starts(lengths)
-    # sequences of like lengths (they ascend) side by side in padded batches that are at least half full
+    # short sequences of like lengths (they ascend) side by side in padded batches that are at least half full
     groups = [[]]
     for b in reversed(range(len(lengths))):
-        if sum(lengths[i] ** 2 for i in groups[-1] + [b]) * 2 < (len(groups[-1]) + 1) * max(lengths[i] for i in groups[-1] + [b]) ** 2:
+        group = [lengths[i] for i in groups[-1] + [b]]
+        if len(group) > 1 and (max(group) > 1024 or sum(n * n for n in group) * 2 < len(group) * max(group) ** 2):
             groups.append([])
         groups[-1].append(b)
     for group in groups:

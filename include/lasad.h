@@ -74,8 +74,8 @@ enum {
     LASAD_OPT_PREFILL_CHUNK = 1,/* CUDA-core prefill chunk length: 0 auto, else 16/32/64          */
     LASAD_OPT_DECODE_TPU = 2,   /* decode: threads per (b,h) state; 0 auto, else 32/64/128/256 */
     LASAD_OPT_WAIT_LIMIT = 3,   /* iteration cap of device-side waits; 0 = library default   */
-    LASAD_OPT_WINDOW_IMPL = 4   /* window attention and its gradient: 0 auto (bf16: 2, f32: 1), 1 CUDA cores,
-                                   2 tensor cores (bf16 only)                                */
+    LASAD_OPT_WINDOW_IMPL = 4   /* window and packed attention and their gradients: 0 auto (bf16: 2, f32: 1),
+                                   1 CUDA cores, 2 tensor cores (bf16 only)                  */
 };
 
 typedef struct lasad_params {
@@ -430,6 +430,103 @@ int lasad_window_attention_step(lasad_ctx* ctx, const lasad_window_params* p, co
  * such caches; slots that no token has reached are not written. */
 int lasad_window_cache_store(lasad_ctx* ctx, const lasad_window_params* p, const void* k, const void* v,
                              const int32_t* lengths, void* k_cache, void* v_cache, void* cuda_stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * A layer that attends to whole sequences: prompts and training on packed sequences, a paged cache in 8 bits,
+ * and one token per sequence against it.  The rules are those of the calls above (alignment, strides, dtypes,
+ * workspaces, graphs, the same bits on every run); d in {32, 64}, Hk divides Hq, query head h reads key head
+ * h / (Hq / Hk).
+ * ---------------------------------------------------------------------------------------------- */
+
+/*
+ * Causal softmax attention over sequences of different lengths that lie end to end in memory:
+ *
+ *     o_t = sum_{s <= t} p_ts v_s ,   p_ts = e^(scale q_t.k_s) / sum_{s <= t} e^(scale q_t.k_s)   (s of t's sequence).
+ *
+ *   q, o [N,Hq,d], k, v [N,Hk,d];  offsets [S + 1] int32 (device), ascending from 0 to at most N: sequence i
+ *   has rows offsets[i] .. offsets[i + 1] - 1 (none where they are equal).  A row that no sequence has (behind the
+ *   last one) is empty: its o and gradients are 0 and its lse is -infinity, and nothing that stands in q, k,
+ *   v, o, do there counts, not even a NaN.  Nor does a row of one sequence count in another's.  (Inside a sequence a
+ *   NaN or an infinity may reach rows ahead of it: a weight of 0 times an infinity is not 0.)  Offsets that do not
+ *   ascend give undefined results, but no access outside the N rows.
+ *   lse [Hq,N] fp32: log of the row's sum of e^(scale q.k); may be NULL in the forward.
+ * Arithmetic and rounding are those of lasad_window_attention (bf16: tensor cores, weights and the gradients of the
+ * scores in bf16 where they enter a product; f32 and LASAD_OPT_WINDOW_IMPL = 1: fp32).
+ * N <= 2^30, S <= 65535.
+ */
+typedef struct lasad_packed_params {
+    int32_t N, S, Hq, Hk, d;
+    int32_t dtype;
+    float scale;
+    int32_t reserved; /* must be 0 */
+    /* element strides of (token, head) */
+    int64_t q_stride[2], k_stride[2], v_stride[2], o_stride[2];
+    int64_t do_stride[2], dq_stride[2], dk_stride[2], dv_stride[2];
+} lasad_packed_params;
+
+int lasad_packed_attention(lasad_ctx* ctx, const lasad_packed_params* p, const void* q, const void* k, const void* v,
+                           const int32_t* offsets, void* o, float* lse, void* cuda_stream);
+/* Bytes of workspace of the backward, or a negative LASAD_ERR_*. */
+int64_t lasad_packed_attention_workspace(lasad_ctx* ctx, const lasad_packed_params* p);
+/* The gradient, from the forward's inputs and its o and lse, and d_o [N,Hq,d]: dq, dk, dv. */
+int lasad_packed_attention_backward(lasad_ctx* ctx, const lasad_packed_params* p, const void* q, const void* k,
+                                    const void* v, const void* o, const float* lse, const void* d_o,
+                                    const int32_t* offsets, void* dq, void* dk, void* dv, void* workspace,
+                                    void* cuda_stream);
+
+/*
+ * A paged cache in 8 bits.  A pool has `pages` pages of `page` tokens (16, 32, 64 or 128) of every key head:
+ *
+ *   k_pages, v_pages [pages,Hk,page,d] e4m3 (strides in bytes of (page, head, slot), channels contiguous)
+ *   k_scales, v_scales [pages,Hk] fp32, positive: what a page's numbers of a head are multiplied by
+ *   block_table [B,table_pages] int32 (device): sequence b keeps its tokens i page .. (i + 1) page - 1 in page
+ *   block_table[b][i].  An entry outside the pool is no page: what would be written there is dropped,
+ *   and its tokens are not seen; so are positions past the table's end.
+ */
+typedef struct lasad_paged_params {
+    int32_t B, N, Hq, Hk, d; /* N: rows of new tokens (append)                                */
+    int32_t dtype;           /* of q, k, v, o                                                 */
+    int32_t page, pages, table_pages;
+    int32_t grid_w, prefix_len, table_rows, flags; /* append: as in lasad_rope_params; flags LASAD_ROPE_* */
+    float scale;             /* attention                                                     */
+    int64_t k_pages_stride[3], v_pages_stride[3];
+    /* element strides of (row, head); o_stride is q_out's in the append */
+    int64_t q_stride[2], k_stride[2], v_stride[2], o_stride[2];
+} lasad_paged_params;
+
+/*
+ * Puts new tokens into the cache, keys rotated by position on the way, and rotates their queries.
+ *
+ *   k, v [N,Hk,d], q, q_out [N,Hq,d] (both or neither may be NULL; q_out may be q)
+ *   pos [B] int32 (device): the position of each sequence's first new token; a sequence with a negative one takes no
+ *   part.  offsets [B + 1] int32 (device) as in lasad_packed_attention, or NULL: N = B, one token each.
+ *   table: fp32 (cos, sin) [table_rows, pairs, 2] with the rules of lasad_qk_norm_rope for positions from `pos`, or
+ *   NULL: k and q are taken as they are (and k may have been turned by lasad_qk_norm_rope).
+ *
+ * Keys turn in 64 bits and are rounded to fp32 once; queries in fp32.  A page and head's scale is a power of two:
+ * the smallest 2^e, -40 <= e <= 40, with max |x| <= 448 2^e over the call's new tokens in it, or, where the page
+ * holds earlier tokens (its first slot is not among the new), the larger of that and the scale that stands there; if
+ * that grows, the earlier tokens are rounded again.  Then x / scale is rounded to e4m3, to nearest, ties to even,
+ * larger ones to 448.  The maximum passes over infinities and NaN; a NaN stays one.
+ * Slots that no new token has are not written, but for that rounding; rows of q_out that no sequence has (or of one that
+ * takes no part) are 0.  A page that is written to must belong to one sequence of the call only (pages
+ * that sequences share are for reading), or its contents are undefined.
+ */
+int lasad_paged_append(lasad_ctx* ctx, const lasad_paged_params* p, const void* k, const void* v, const void* q,
+                       const float* table, const int32_t* offsets, const int32_t* pos, const int32_t* block_table,
+                       void* k_pages, void* v_pages, float* k_scales, float* v_scales, void* q_out, void* cuda_stream);
+
+/*
+ * Softmax attention of one token per sequence, q, o [B,Hq,d], over the tokens 0 .. pos[b] that the cache holds
+ * (the token's own among them: append it first).  lse [B,Hq] fp32 or NULL.  A sequence with a negative position, or
+ * that sees no page, has o = 0 and lse = -infinity.  Scores, statistics and sums are fp32; with bf16 the weights
+ * are rounded to fp16 where they meet the values (2^-11), with f32 nothing is rounded below 22 bits.
+ * table_pages * page <= 2^30.
+ */
+int64_t lasad_paged_attention_workspace(lasad_ctx* ctx, const lasad_paged_params* p);
+int lasad_paged_attention(lasad_ctx* ctx, const lasad_paged_params* p, const void* q, const void* k_pages,
+                          const void* v_pages, const float* k_scales, const float* v_scales, const int32_t* block_table,
+                          const int32_t* pos, void* o, float* lse, void* workspace, void* cuda_stream);
 
 /* After the caller has synchronised the stream: 0, or LASAD_ERR_TIMEOUT if a kernel gave up a
  * bounded wait since the last query (the flag is cleared by the query).  Synchronous copy. */

@@ -14,6 +14,7 @@ import torch
 
 from . import build as _build
 from . import mixers as _mixers
+from . import sequences as _sequences
 from .marshal import (LASAD_BF16, LASAD_F32, _check_cuda, _dtype_code, _empty, _ptr, _raw_stream, _stream,  # noqa: F401
                       _strides3, _strides_decode)
 from .mixers import rope_table  # noqa: F401
@@ -34,7 +35,7 @@ EXPORTS = (
     "lasad_decode_step", "lasad_decode_step_pos", "lasad_forward_gated", "lasad_decode_step_gated",
     "lasad_forward_fused", "lasad_decode_step_fused",
     "lasad_last_device_status", "lasad_last_cuda_error", "lasad_launch_count", "lasad_strerror",
-) + tuple(_mixers.PROTOTYPES)
+) + tuple(_mixers.PROTOTYPES) + tuple(_sequences.PROTOTYPES)
 
 
 class LasadParams(ctypes.Structure):
@@ -104,7 +105,7 @@ def load_library() -> ctypes.CDLL:
         lib.lasad_launch_count.argtypes = [vp]
         lib.lasad_strerror.restype = ctypes.c_char_p
         lib.lasad_strerror.argtypes = [i32]
-        for name, (restype, argtypes) in _mixers.PROTOTYPES.items():
+        for name, (restype, argtypes) in (*_mixers.PROTOTYPES.items(), *_sequences.PROTOTYPES.items()):
             getattr(lib, name).restype = restype
             getattr(lib, name).argtypes = argtypes
         _lib = lib
@@ -139,7 +140,7 @@ def _params(kind, q, k, v, o, grid_w, prefix_len, t0, scale):
     return p
 
 
-class Lasad(_mixers.Mixers):
+class Lasad(_mixers.Mixers, _sequences.Sequences):
     """A ``lasad_ctx`` bound to one CUDA device."""
 
     def __init__(self, device: int | None = None):

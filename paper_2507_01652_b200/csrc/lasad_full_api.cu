@@ -63,6 +63,13 @@ int packed_args(lasad_ctx* ctx, const lasad_packed_params* p, bool backward, las
     return LASAD_OK;
 }
 
+// 1: CUDA cores, 2: tensor cores (LASAD_OPT_WINDOW_IMPL)
+int packed_impl(const lasad_ctx* ctx, const lasad::PackedArgs& a)
+{
+    if (ctx->opt_window_impl == 0) return a.bf16 ? 2 : 1;
+    return ctx->opt_window_impl == 2 && !a.bf16 ? LASAD_ERR_UNSUPPORTED : ctx->opt_window_impl;
+}
+
 // Strides in bytes of (page, head, slot).
 bool pages_ok(const int64_t* s, const lasad_paged_params* p, long long (&to)[3])
 {
@@ -119,7 +126,9 @@ int lasad_packed_attention(lasad_ctx* ctx, const lasad_packed_params* p, const v
     if (!q || !k || !v || !offsets || !o || !all({q, k, v, o}, 16) || !all({offsets, lse}, 4)) return LASAD_ERR_INVALID_ARG;
     a.q = q, a.k = k, a.v = v, a.o = o, a.lse = lse, a.offsets = offsets;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    return launched(ctx, lasad::launch_packed_forward_simt(a, st), 1);
+    const int impl = packed_impl(ctx, a);
+    if (impl < 0) return impl;
+    return launched(ctx, impl == 2 ? lasad::launch_packed_forward_tc(a, st) : lasad::launch_packed_forward_simt(a, st), 1);
 }
 
 int64_t lasad_packed_attention_workspace(lasad_ctx* ctx, const lasad_packed_params* p)

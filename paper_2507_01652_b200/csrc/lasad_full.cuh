@@ -74,6 +74,7 @@ __host__ __device__ inline long long packed_stat_at(const PackedArgs& a, int h, 
 }
 inline size_t packed_workspace_bytes(const PackedArgs& a) { return (size_t)packed_stat_at(a, a.Hq, 0) * sizeof(float); }
 cudaError_t launch_packed_forward_tc(const PackedArgs& a, cudaStream_t st);       // bf16
+cudaError_t launch_packed_backward_tc(const PackedArgs& a, cudaStream_t st);      // two launches
 cudaError_t launch_packed_forward_simt(const PackedArgs& a, cudaStream_t st);
 cudaError_t launch_packed_backward_simt(const PackedArgs& a, cudaStream_t st);   // two launches
 

@@ -151,7 +151,9 @@ int lasad_packed_attention_backward(lasad_ctx* ctx, const lasad_packed_params* p
     a.q = q, a.k = k, a.v = v, a.o = const_cast<void*>(o), a.lse = const_cast<float*>(lse), a.dout = d_o, a.offsets = offsets;
     a.dq = dq, a.dk = dk, a.dv = dv, a.ws = static_cast<float*>(workspace);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    return launched(ctx, lasad::launch_packed_backward_simt(a, st), 2);
+    const int impl = packed_impl(ctx, a);
+    if (impl < 0) return impl;
+    return launched(ctx, impl == 2 ? lasad::launch_packed_backward_tc(a, st) : lasad::launch_packed_backward_simt(a, st), 2);
 }
 
 int lasad_paged_append(lasad_ctx* ctx, const lasad_paged_params* p, const void* k, const void* v, const void* q,

@@ -54,7 +54,7 @@ struct Smem {
     unsigned long long q_full[2], q_free[2];               // a unit's Q has landed; its last S has been made (both groups)
     unsigned long long full[kStages], free[kStages];       // a tile's K and V have landed; both groups are done with them
     unsigned long long s_full[kGroups][2];                 // S of a tile is in TMEM, and its P's place is free
-    unsigned long long p_ready[kGroups][2];                // S has been read and P is in TMEM (128 arrivals)
+    unsigned long long p_ready[kGroups][2];                // S has been read and P is in TMEM (4 warps)
     // P V has been added: of even and odd tiles, as a warp that has seen S of tile J knows of tile J - 2's product and not of
     // the next one's (a barrier's parity tells only two neighbouring phases apart)
     unsigned long long o_done[kGroups][2];
@@ -396,7 +396,9 @@ __device__ __forceinline__ void softmax_rows(const Params& p, Smem& sm, int g, i
             }
             tmem_wait_st();
             tc_fence_before();
-            mbar_arrive(&sm.p_ready[g][J & 1]);
+            // (one arrival for the warp: 32 of them are made one after another)
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.p_ready[g][J & 1]);
         }
         if (!ok) break;
         tile += max(w.tiles[0], w.tiles[1]);
@@ -451,7 +453,7 @@ packed_forward_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
         for (int g = 0; g < kGroups; ++g) {
             for (int s = 0; s < 2; ++s) {
                 mbar_init(&sm.s_full[g][s], 1);
-                mbar_init(&sm.p_ready[g][s], kRows);
+                mbar_init(&sm.p_ready[g][s], 4);
                 mbar_init(&sm.o_done[g][s], 1);
             }
             mbar_init(&sm.drain[g], 1);
@@ -498,20 +500,13 @@ packed_forward_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
     }
 }
 
-// [N,H,d] with element strides of (token, head) -> the rows map's (d, h, t, b) with one batch element
-bool encode_packed(CUtensorMap* map, const void* base, int d, int N, int H, const long long (&s)[2], int rows)
-{
-    const long long strides[3] = {0, s[0], s[1]};
-    return encode_rows_map(map, base, d, 1, N, H, strides, rows);
-}
-
 }  // namespace
 
 cudaError_t launch_packed_forward_tc(const PackedArgs& a, cudaStream_t st)
 {
     CUtensorMap mq, mk, mv;
-    if (!encode_packed(&mq, a.q, a.d, a.N, a.Hq, a.qs, kRows) || !encode_packed(&mk, a.k, a.d, a.N, a.Hk, a.ks, kCols) ||
-        !encode_packed(&mv, a.v, a.d, a.N, a.Hk, a.vs, kCols))
+    if (!encode_packed_map(&mq, a.q, a.d, a.N, a.Hq, a.qs, kRows) || !encode_packed_map(&mk, a.k, a.d, a.N, a.Hk, a.ks, kCols) ||
+        !encode_packed_map(&mv, a.v, a.d, a.N, a.Hk, a.vs, kCols))
         return cudaErrorInvalidValue;
     static bool done[64];
     const size_t smem = sizeof(Smem) + 1024;

@@ -27,6 +27,13 @@ inline bool encode_rows_map(CUtensorMap* map, const void* base, int d, int B, in
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// [N,H,d] bf16 with element strides of (token, head): the same map with one batch element.
+inline bool encode_packed_map(CUtensorMap* map, const void* base, int d, int N, int H, const long long (&s)[2], int rows)
+{
+    const long long strides[3] = {0, s[0], s[1]};
+    return encode_rows_map(map, base, d, 1, N, H, strides, rows);
+}
+
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr unsigned kDrainLimit = 1u << 26;
 

@@ -3,11 +3,12 @@
 //     o = sum_j p_j v_j ,   p_j = e^(scale q.k_j) / sum   over the tokens 0 .. pos of the sequence.
 //
 // Bound by reading the cache once, 2 d bytes a token and key head.  A warp takes steps of 16 tokens, straight from
-// memory into the fragments of two products on mma.sync.m16n8k16 (the rows are the query heads that share
-// the key head: 16 of them, of which few are used, so the tensor cores have time to spare and tcgen05's 128 rows
-// would only add a way through shared memory).  e4m3 numbers are exact in fp16, so keys and values enter
-// without a rounding; the page's key scale multiplies the fp32 score.  The order of a product's inner index is
-// free, so a lane reads 16 neighbouring channels of a key and 8 of a value.
+// memory into the fragments of two products on mma.sync.m16n8k16 (tokens are the rows of the first, channels those of
+// the second; the columns are the query heads that share the key head, 8 at a time, of which few are used, so the
+// tensor cores have time to spare and tcgen05's 128 rows would only add a way through shared memory).  e4m3 numbers are
+// exact in fp16, so keys and values enter without a rounding; the page's key scale multiplies the fp32 score.  The order
+// of a product's inner index is free, and so is that of its rows, so a lane reads 16 neighbouring channels of a
+// key and 8 of a value.
 //
 // The page's value scale goes into the exponent: with x_j = scale q.k_j log2(e) + log2 s_j a warp sums
 //
@@ -15,9 +16,9 @@
 //
 // so that w stays in the range of fp16 however far the scales of two pages are apart.  M lies 11 below a lagging
 // maximum, which moves only when some row has grown by more than 4: w is at most 2^15, and it keeps its eleven
-// digits down to 2^-25 of the largest and some down to 2^-35.  w is rounded to fp16 (2^-11 of each term) where q is bf16; where q is
-// fp32, q and w enter as sums of two fp16 numbers (22 bits).  q is brought near 1 by a power of two first, so that
-// fp16 holds it.
+// digits down to 2^-25 of the largest and some down to 2^-35.  w is rounded to fp16 (2^-11 of each term) where q is bf16;
+// where q is fp32, q and w enter as sums of two fp16 numbers (22 bits).  q is brought near 1 by a power of two first,
+// so that fp16 holds it.
 //
 // The tokens of a sequence are cut into parts where there are few (sequence, key head) pairs; then the parts'
 // (M, l, O) go to memory and a second kernel joins them.
@@ -27,13 +28,14 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
+#include <type_traits>
 
 namespace lasad {
 namespace {
 
-constexpr int kWarps = 4, kStep = 16, kMinPart = 256;    // kMinPart: tokens of a part, at least
-constexpr int kAhead = 2;                                // steps of a warp in flight beside the one it works on
-constexpr float kLift = 11.0f, kLag = 4.0f;              // of the largest x over M; how far it may be over that
+constexpr int kCtaWarps = 4, kStep = 16, kMinPart = 256;  // kMinPart: tokens of a part, at least
+constexpr int kColTiles = 3;                              // columns of a warp: at most 24 query heads
+constexpr float kLift = 11.0f, kLag = 4.0f;               // of the largest x over M; how far it may be over that
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
@@ -60,6 +62,13 @@ __device__ __forceinline__ uint32_t rest_f16(float lo, float hi, uint32_t packed
     const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&packed));
     return pack_f16(lo - f.x, hi - f.y);
 }
+// An 8 x 8 tile of fp16 numbers, lane 4 i + j with (i, 2 j) and (i, 2 j + 1), turned over.
+__device__ __forceinline__ uint32_t transposed(uint32_t x)
+{
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
+}
 
 // The tokens of a sequence and how they are cut: part p has tokens p * size .. of n.
 struct Cut {
@@ -75,47 +84,122 @@ __device__ __forceinline__ Cut cut_of(const PagedArgs& a, int b)
     return c;
 }
 
-// A lane's share of 16 tokens: of tokens g and 8 + g the keys' channels t D / 4 .. (g = lane / 4, t = lane % 4), of tokens
-// 2 t, 2 t + 1, 8 + 2 t, 9 + 2 t the values' channels g D / 8 .. .
+// A lane's share of 16 tokens (g = lane / 4, t = lane % 4): of tokens g and 8 + g the keys' channels t D / 4 .. , of tokens 2 t,
+// 2 t + 1, 8 + 2 t, 9 + 2 t the values' channels g D / 8 .. .
 template <int D> struct Step {
     uint32_t k[2][D / 16], v[4][D / 32];
-    float ks, lv, iv;            // the key scale, log2 of the value scale and its reciprocal; ks < 0: no such page
-    int at;                      // its first token
 };
 
-// PAIR: fp32 queries.  LOW: at most 8 query heads, rows 8 to 15 are empty.
-template <int D, bool PAIR, bool LOW>
-__global__ void __launch_bounds__(32 * kWarps) paged_attention_kernel(const PagedArgs a, int row_tiles)
+template <int D> __device__ __forceinline__ void load_key(uint32_t (&to)[D / 16], const unsigned char* at)
+{
+    if constexpr (D == 64) {
+        const uint4 v = *reinterpret_cast<const uint4*>(at);
+        to[0] = v.x, to[1] = v.y, to[2] = v.z, to[3] = v.w;
+    } else {
+        const uint2 v = *reinterpret_cast<const uint2*>(at);
+        to[0] = v.x, to[1] = v.y;
+    }
+}
+template <int D> __device__ __forceinline__ void load_value(uint32_t (&to)[D / 32], const unsigned char* at)
+{
+    if constexpr (D == 64) {
+        const uint2 v = *reinterpret_cast<const uint2*>(at);
+        to[0] = v.x, to[1] = v.y;
+    } else {
+        to[0] = *reinterpret_cast<const uint32_t*>(at);
+    }
+}
+
+// A unit is a sequence, a key head, up to 8 NR of its query heads and a part of the tokens; WARPS warps have it.  PAIR:
+// fp32 queries.  AHEAD: steps of a warp in flight beside the one it works on.
+template <int D, bool PAIR, int NR, int WARPS, int AHEAD>
+__global__ void __launch_bounds__(32 * kCtaWarps) paged_attention_kernel(const PagedArgs a, int col_blocks)
 {
     constexpr int KK = D / 16;                               // inner steps of q.k; words of a lane's key piece
-    constexpr int DN = D / 8;                                // column tiles of O
-    __shared__ float part[kWarps][16][D + 2];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    constexpr int MT = D / 16;                               // row tiles of O
+    __shared__ float part[WARPS > 1 ? WARPS : 1][WARPS > 1 ? 8 * NR : 1][D + 2];
+    const int lane = threadIdx.x & 31, warp = WARPS > 1 ? threadIdx.x >> 5 : 0, g = lane >> 2, t = lane & 3;
     const int G = a.Hq / a.Hk;
-    // blockIdx.x = ((part * B + sequence) * Hk + key head) * row_tiles + row tile
-    int rest = blockIdx.x;
-    const int rt = rest % row_tiles;
-    rest /= row_tiles;
-    const int hk = rest % a.Hk;
-    rest /= a.Hk;
-    const int b = rest % a.B, p = rest / a.B;
-    const int rows = min(16, G - rt * 16), h0 = hk * G + rt * 16;
+    // unit = ((part * B + sequence) * Hk + key head) * col_blocks + block of query heads
+    long long unit = WARPS > 1 ? blockIdx.x : (long long)blockIdx.x * kCtaWarps + (threadIdx.x >> 5);
+    const int cb = (int)(unit % col_blocks);
+    unit /= col_blocks;
+    const int hk = (int)(unit % a.Hk);
+    unit /= a.Hk;
+    const int b = (int)(unit % a.B), p = (int)(unit / a.B);
+    const int heads = min(8 * NR, G - cb * 8 * NR), h0 = hk * G + cb * 8 * NR;
     pdl_wait();
+    if (p >= a.splits) return;                               // (behind the last unit)
     const Cut cut = cut_of(a, b);
     if (p >= max(cut.parts, 1)) return;
     const int lo = p * cut.size, hi = min(cut.n, lo + cut.size);
 
-    // q as fp16 fragments: inner step kk, register r: row g + 8 (r & 1), channels t D / 4 + 4 kk + 2 (r >> 1) and the next
-    uint32_t qa[KK][4], ql[PAIR ? KK : 1][4];
-    float factor[2];                                         // scale log2(e) and what q was divided by
+    // The warp's steps: number i is at lo + (i WARPS + warp) kStep.  Pages and scales of 32 of them are fetched at a
+    // time, one by each lane, a batch ahead of the one that is worked on.
+    const int steps = (max(hi - lo, 0) + kStep - 1) / kStep, mine = (steps - warp + WARPS - 1) / WARPS;
+    const int* ids = a.block_table + (long long)b * a.table_pages;
+    struct Pages {
+        int id;
+        float ks, vs;                                        // the scales
+    };
+    auto fetch_pages = [&](int i) {                          // of steps i .. i + 31
+        Pages f{-1, 0.0f, 1.0f};
+        if (i + lane < mine) f.id = ids[(lo + ((i + lane) * WARPS + warp) * kStep) / a.page];
+        if (f.id >= a.pages) f.id = -1;
+        if (f.id >= 0) {
+            f.ks = a.kscale[(long long)f.id * a.Hk + hk];
+            f.vs = a.vscale[(long long)f.id * a.Hk + hk];
+        }
+        return f;
+    };
+    Pages now = fetch_pages(0), next = fetch_pages(32);
+    int batch = 0;                                           // the first step of `now`
+    const unsigned char* const at_k = a.kp + hk * a.kps[1] + g * a.kps[2] + t * (D / 4);
+    const unsigned char* const at_v = a.vp + hk * a.vps[1] + 2 * t * a.vps[2] + g * (D / 8);
+    auto load = [&](Step<D>& s, int i) {
+        const int page = __shfl_sync(0xffffffffu, i - batch < 32 ? now.id : next.id, i & 31);
+        const int at = lo + (i * WARPS + warp) * kStep, slot = at & (a.page - 1);
+        const int live = page >= 0 && i < mine ? hi - at : 0;        // tokens of the step that count
+        const unsigned char* k = at_k + page * a.kps[0] + slot * a.kps[2];
+        const unsigned char* v = at_v + page * a.vps[0] + slot * a.vps[2];
+        if (live >= kStep) {
+            load_key<D>(s.k[0], k);
+            load_key<D>(s.k[1], k + 8 * a.kps[2]);
+            load_value<D>(s.v[0], v);
+            load_value<D>(s.v[1], v + a.vps[2]);
+            load_value<D>(s.v[2], v + 8 * a.vps[2]);
+            load_value<D>(s.v[3], v + 9 * a.vps[2]);
+        } else {
+            // (what does not count is 0, whatever stands there: a weight of 0 times a NaN is not 0)
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+            for (int n = 0; n < 2; ++n) {
+#pragma unroll
+                for (int e = 0; e < D / 16; ++e) s.k[n][e] = 0u;
+                if (8 * n + g < live) load_key<D>(s.k[n], k + 8 * n * a.kps[2]);
+            }
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                const int token = (n & 1) + 8 * (n >> 1);
+#pragma unroll
+                for (int e = 0; e < D / 32; ++e) s.v[n][e] = 0u;
+                if (2 * t + token < live) load_value<D>(s.v[n], v + token * a.vps[2]);
+            }
+        }
+    };
+    Step<D> ring[AHEAD + 1];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) load(ring[i], i);
+
+    // q as fp16 fragments: inner step kk, register r: column g (query head), channels t D / 4 + 4 kk + 2 r and the next
+    uint32_t qb[NR][KK][2], ql[PAIR ? NR : 1][PAIR ? KK : 1][2];
+    float mine_factor[NR];                                   // scale log2(e) and what q was divided by, of column g
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
         float x[D / 4], top = 0.0f;
 #pragma unroll
         for (int e = 0; e < D / 4; ++e) x[e] = 0.0f;
-        const int row = g + 8 * i;
-        if ((!LOW || i == 0) && row < rows) {
-            const long long at = b * a.qs[0] + (h0 + row) * a.qs[1] + t * (D / 4);
+        if (8 * n + g < heads) {
+            const long long at = b * a.qs[0] + (h0 + 8 * n + g) * a.qs[1] + t * (D / 4);
             if (PAIR) {
 #pragma unroll
                 for (int e = 0; e < D / 16; ++e) {
@@ -139,242 +223,255 @@ __global__ void __launch_bounds__(32 * kWarps) paged_attention_kernel(const Page
         // |q| < 2 after division by 2^e (a power that fp32 has, and its reciprocal too)
         const int e2 = max(-120, min(120, (int)(__float_as_uint(top) >> 23) - 127));
         const float down = __uint_as_float((uint32_t)(127 - e2) << 23);
-        factor[i] = a.scale * kLog2e * __uint_as_float((uint32_t)(127 + e2) << 23);
+        mine_factor[n] = a.scale * kLog2e * __uint_as_float((uint32_t)(127 + e2) << 23);
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
                 const float u = x[4 * kk + 2 * r] * down, v = x[4 * kk + 2 * r + 1] * down;
-                qa[kk][2 * r + i] = pack_f16(u, v);
-                if (PAIR) ql[kk][2 * r + i] = rest_f16(u, v, qa[kk][2 * r + i]);
+                qb[n][kk][r] = pack_f16(u, v);
+                if (PAIR) ql[n][kk][r] = rest_f16(u, v, qb[n][kk][r]);
             }
     }
+    // scores have columns 2 t and 2 t + 1 (i) in a lane
+    float factor[NR][2], m[NR][2], l[NR][2], o[NR][MT][4];
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            factor[n][i] = __shfl_sync(0xffffffffu, mine_factor[n], 4 * (2 * t + i));
+            m[n][i] = -INFINITY;
+            l[n][i] = 0.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < MT; ++k) o[n][k][0] = o[n][k][1] = o[n][k][2] = o[n][k][3] = 0.0f;
+    }
 
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f}, o[DN][4];
+    float lv = log2f(now.vs), iv = 1.0f / now.vs;            // of the value scales: log2 and reciprocal
+    auto work = [&](const Step<D>& s, int i) {
+        const float step_ks = __shfl_sync(0xffffffffu, now.ks, i & 31), step_lv = __shfl_sync(0xffffffffu, lv, i & 31);
+        const float step_iv = __shfl_sync(0xffffffffu, iv, i & 31);
+        const int page = __shfl_sync(0xffffffffu, now.id, i & 31), live = page < 0 ? 0 : hi - (lo + (i * WARPS + warp) * kStep);
+        // scores: c[0..1] of token g, c[2..3] of token 8 + g
+        float c[NR][4];
 #pragma unroll
-    for (int n = 0; n < DN; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.0f;
-
-    // The warp's steps: number i is at lo + (i kWarps + warp) kStep.  Pages and scales of 32 of them are fetched at a
-    // time, one by each lane.
-    const int steps = (max(hi - lo, 0) + kStep - 1) / kStep, mine = (steps - warp + kWarps - 1) / kWarps;
-    const int* ids = a.block_table + (long long)b * a.table_pages;
-    int id = -1;
-    float ks = 0.0f, vs = 1.0f;
-    auto fetch_pages = [&](int i) {                          // steps i .. i + 31
-        id = -1;
-        if (i + lane < mine) id = ids[(lo + ((i + lane) * kWarps + warp) * kStep) / a.page];
-        if (id >= a.pages) id = -1;
-        if (id >= 0) {
-            ks = a.kscale[(long long)id * a.Hk + hk];
-            vs = a.vscale[(long long)id * a.Hk + hk];
-        }
-    };
-    auto load = [&](Step<D>& s, int i) {
-        if ((i & 31) == 0) fetch_pages(i);
-        const int page = __shfl_sync(0xffffffffu, id, i & 31);
-        s.ks = __shfl_sync(0xffffffffu, ks, i & 31);
-        const float v = __shfl_sync(0xffffffffu, vs, i & 31);
-        s.lv = log2f(v);
-        s.iv = 1.0f / v;
-        s.at = lo + (i * kWarps + warp) * kStep;
-        const int slot = s.at % a.page, live = page >= 0 && i < mine ? hi - s.at : 0;    // tokens of the step that count
-        if (live <= 0) s.at = hi;
+        for (int n = 0; n < NR; ++n) c[n][0] = c[n][1] = c[n][2] = c[n][3] = 0.0f;
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            const unsigned char* at = a.kp + page * a.kps[0] + hk * a.kps[1] + (slot + 8 * n + g) * a.kps[2] + t * (D / 4);
-            if (8 * n + g < live) {
-                if constexpr (D == 64) {
-                    const uint4 v = *reinterpret_cast<const uint4*>(at);
-                    s.k[n][0] = v.x, s.k[n][1] = v.y, s.k[n][2] = v.z, s.k[n][3] = v.w;
-                } else {
-                    const uint2 v = *reinterpret_cast<const uint2*>(at);
-                    s.k[n][0] = v.x, s.k[n][1] = v.y;
-                }
-            } else {
+        for (int kk = 0; kk < KK; ++kk) {
+            const uint32_t f[4] = {f16_of(s.k[0][kk]), f16_of(s.k[1][kk]), f16_of(s.k[0][kk] >> 16), f16_of(s.k[1][kk] >> 16)};
 #pragma unroll
-                for (int e = 0; e < D / 16; ++e) s.k[n][e] = 0u;
+            for (int n = 0; n < NR; ++n) {
+                mma16816(c[n], f, qb[n][kk][0], qb[n][kk][1]);
+                if (PAIR) mma16816(c[n], f, ql[n][kk][0], ql[n][kk][1]);
             }
         }
+        bool grow = false;
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {
-            const int token = 2 * t + (n & 1) + 8 * (n >> 1);
-            const unsigned char* at = a.vp + page * a.vps[0] + hk * a.vps[1] + (slot + token) * a.vps[2] + g * (D / 8);
-            if (token < live) {
-                if constexpr (D == 64) {
-                    const uint2 v = *reinterpret_cast<const uint2*>(at);
-                    s.v[n][0] = v.x, s.v[n][1] = v.y;
-                } else {
-                    s.v[n][0] = *reinterpret_cast<const uint32_t*>(at);
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+            for (int i2 = 0; i2 < 2; ++i2) {
+                const float f = step_ks * factor[n][i2];
+                c[n][i2] = fmaf(c[n][i2], f, step_lv);
+                c[n][2 + i2] = fmaf(c[n][2 + i2], f, step_lv);
+                if (live < kStep) {
+                    if (g >= live) c[n][i2] = -INFINITY;
+                    if (8 + g >= live) c[n][2 + i2] = -INFINITY;
                 }
-            } else {
-#pragma unroll
-                for (int e = 0; e < D / 32; ++e) s.v[n][e] = 0u;
+                grow = grow || fmaxf(c[n][i2], c[n][2 + i2]) > m[n][i2] + (kLift + kLag);
             }
-        }
-    };
-    auto work = [&](const Step<D>& s) {
-        // scores: c[n][0..1] of row g and tokens 8 n + 2 t, + 1, c[n][2..3] of row g + 8
-        float c[2][4];
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            c[n][0] = c[n][1] = c[n][2] = c[n][3] = 0.0f;
-#pragma unroll
-            for (int kk = 0; kk < KK; ++kk) {
-                const uint32_t b0 = f16_of(s.k[n][kk]), b1 = f16_of(s.k[n][kk] >> 16);
-                mma16816(c[n], qa[kk], b0, b1);
-                if (PAIR) mma16816(c[n], ql[kk], b0, b1);
-            }
-        }
-        const int live = hi - s.at;
-        float top[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-        for (int i = 0; i < (LOW ? 1 : 2); ++i) {
-            const float f = s.ks * factor[i];
-#pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    float& x = c[n][2 * i + e];
-                    x = 8 * n + 2 * t + e < live ? fmaf(x, f, s.lv) : -INFINITY;
-                    top[i] = fmaxf(top[i], x);
-                }
-        }
-        bool grow = top[0] > m[0] + (kLift + kLag);
-        if (!LOW) grow = grow || top[1] > m[1] + (kLift + kLag);
         if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
-            for (int i = 0; i < (LOW ? 1 : 2); ++i) {
-                top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
-                top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
-                const float now = fmaxf(m[i], top[i] - kLift), f = now == m[i] ? 1.0f : tcx::ex2_approx(m[i] - now);
-                m[i] = now;
-                l[i] *= f;
+            for (int n = 0; n < NR; ++n)
 #pragma unroll
-                for (int n = 0; n < DN; ++n) o[n][2 * i] *= f, o[n][2 * i + 1] *= f;
+                for (int i2 = 0; i2 < 2; ++i2) {
+                    float top = fmaxf(c[n][i2], c[n][2 + i2]);
+#pragma unroll
+                    for (int k = 4; k <= 16; k <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
+                    const float now = fmaxf(m[n][i2], top - kLift), f = now == m[n][i2] ? 1.0f : tcx::ex2_approx(m[n][i2] - now);
+                    m[n][i2] = now;
+                    l[n][i2] *= f;
+#pragma unroll
+                    for (int k = 0; k < MT; ++k) o[n][k][i2] *= f, o[n][k][2 + i2] *= f;
+                }
+        }
+        uint32_t w[NR][2], wl[PAIR ? NR : 1][2];
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+            const float b0 = m[n][0] == -INFINITY ? 0.0f : m[n][0], b1 = m[n][1] == -INFINITY ? 0.0f : m[n][1];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const float x0 = tcx::ex2_approx(c[n][2 * k] - b0), x1 = tcx::ex2_approx(c[n][2 * k + 1] - b1);
+                l[n][0] = fmaf(x0, step_iv, l[n][0]);
+                l[n][1] = fmaf(x1, step_iv, l[n][1]);
+                const uint32_t packed = pack_f16(x0, x1);
+                w[n][k] = transposed(packed);                // tokens 8 k + 2 t, + 1 of column g
+                if (PAIR) wl[n][k] = transposed(rest_f16(x0, x1, packed));
             }
         }
-        uint32_t w[4] = {0u, 0u, 0u, 0u}, wl[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-        for (int i = 0; i < (LOW ? 1 : 2); ++i) {
-            const float base = m[i] == -INFINITY ? 0.0f : m[i];
-#pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                const float x0 = tcx::ex2_approx(c[n][2 * i] - base), x1 = tcx::ex2_approx(c[n][2 * i + 1] - base);
-                l[i] = fmaf(x0 + x1, s.iv, l[i]);
-                w[2 * n + i] = pack_f16(x0, x1);
-                if (PAIR) wl[2 * n + i] = rest_f16(x0, x1, w[2 * n + i]);
-            }
-        }
-        // O += w V: register pairs (token 2 t, 2 t + 1) and (8 + 2 t, 9 + 2 t) of channel g D / 8 + n
+        // O += V^T w: row tile 2 q + half has channels g D / 8 + 4 q + 2 half (rows g) and the next (rows 8 + g)
 #pragma unroll
         for (int q = 0; q < D / 32; ++q)
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const uint32_t sel = half ? 0x7362u : 0x5140u;
                 const uint32_t x = __byte_perm(s.v[0][q], s.v[1][q], sel), y = __byte_perm(s.v[2][q], s.v[3][q], sel);
+                const uint32_t f[4] = {f16_of(x), f16_of(x >> 16), f16_of(y), f16_of(y >> 16)};
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const uint32_t b0 = f16_of(k ? x >> 16 : x), b1 = f16_of(k ? y >> 16 : y);
-                    float (&acc)[4] = o[4 * q + 2 * half + k];
-                    mma16816(acc, w, b0, b1);
-                    if (PAIR) mma16816(acc, wl, b0, b1);
+                for (int n = 0; n < NR; ++n) {
+                    mma16816(o[n][2 * q + half], f, w[n][0], w[n][1]);
+                    if (PAIR) mma16816(o[n][2 * q + half], f, wl[n][0], wl[n][1]);
                 }
             }
     };
-    Step<D> ring[kAhead + 1];
+    for (int i = 0; i < mine; i += AHEAD + 1) {
+        if (i - batch == 32) {
+            now = next;
+            batch = i;
+            lv = log2f(now.vs), iv = 1.0f / now.vs;
+            next = fetch_pages(i + 32);
+        }
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) load(ring[i], i);
-    for (int i = 0; i < mine; i += kAhead + 1) {
-#pragma unroll
-        for (int k = 0; k <= kAhead; ++k) {
+        for (int k = 0; k <= AHEAD; ++k) {
             if (i + k >= mine) break;
-            load(ring[(k + kAhead) % (kAhead + 1)], i + k + kAhead);
-            work(ring[k]);
+            load(ring[(k + AHEAD) % (AHEAD + 1)], i + k + AHEAD);
+            work(ring[k], i + k);
         }
     }
+#pragma unroll
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int k = 4; k <= 16; k <<= 1) l[n][i] += __shfl_xor_sync(0xffffffffu, l[n][i], k);
 
-    // the warps' parts meet in shared memory
+    // M, l and O of query head `col` of the unit's: a lane has E neighbouring channels from d on
+    auto finish = [&](int col, int d, float M, float L, const float* O, auto count) {
+        constexpr int E = decltype(count)::value;
+        const int h = h0 + col;
+        if (a.splits > 1) {
+            float* to = a.ws + (((long long)b * a.Hq + h) * a.splits + p) * (D + 2);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
-        l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
-        float* to = part[warp][g + 8 * i];
-        if (t == 0) to[D] = m[i], to[D + 1] = l[i];
-#pragma unroll
-        for (int n = 0; n < DN; ++n) {
-            to[2 * t * (D / 8) + n] = o[n][2 * i];
-            to[(2 * t + 1) * (D / 8) + n] = o[n][2 * i + 1];
+            for (int e = 0; e < E; e += 2) *reinterpret_cast<float2*>(to + d + e) = make_float2(O[e], O[e + 1]);
+            if (d == 0) *reinterpret_cast<float2*>(to + D) = make_float2(M, L);
+            return;
         }
-    }
-    __syncthreads();
-    for (int e = threadIdx.x; e < rows * D; e += 32 * kWarps) {
-        const int row = e / D, d = e - row * D;
-        float M = -INFINITY, L = 0.0f, O = 0.0f;
+        const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+        const long long at = b * a.os[0] + h * a.os[1] + d;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) M = fmaxf(M, part[w][row][D]);
+        for (int e = 0; e < E; e += 2) {
+            const float x = L == 0.0f ? 0.0f : O[e] * inv, y = L == 0.0f ? 0.0f : O[e + 1] * inv;
+            if (PAIR) *reinterpret_cast<float2*>(static_cast<float*>(a.o) + at + e) = make_float2(x, y);
+            else *reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(a.o) + at + e) = tcx::pack_bf16(x, y);
+        }
+        if (d == 0 && a.lse) a.lse[(long long)b * a.Hq + h] = L == 0.0f ? -INFINITY : M * kLn2 + logf(L);
+    };
+#pragma unroll
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            float x[D / 8];                                  // channels g D / 8 .. of column 8 n + 2 t + i
+#pragma unroll
+            for (int k = 0; k < MT; ++k) x[2 * k] = o[n][k][i], x[2 * k + 1] = o[n][k][2 + i];
+            const int col = 8 * n + 2 * t + i;
+            if (WARPS == 1) {
+                if (col < heads) finish(col, g * (D / 8), m[n][i], l[n][i], x, std::integral_constant<int, D / 8>{});
+            } else {
+                float* to = part[warp][col];
+#pragma unroll
+                for (int e = 0; e < D / 8; e += 2) *reinterpret_cast<float2*>(to + g * (D / 8) + e) = make_float2(x[e], x[e + 1]);
+                if (g == 0) *reinterpret_cast<float2*>(to + D) = make_float2(m[n][i], l[n][i]);
+            }
+        }
+    if (WARPS == 1) return;
+    // the warps' parts meet in shared memory
+    __syncthreads();
+    for (int e = threadIdx.x; e < heads * (D / 2); e += 32 * WARPS) {
+        const int col = e / (D / 2), d = 2 * (e - col * (D / 2));
+        float M = -INFINITY, L = 0.0f, O[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) M = fmaxf(M, part[w][col][D]);
         const float base = M == -INFINITY ? 0.0f : M;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            const float f = tcx::ex2_approx(part[w][row][D] - base);
-            L = fmaf(part[w][row][D + 1], f, L);
-            O = fmaf(part[w][row][d], f, O);
+        for (int w = 0; w < WARPS; ++w) {
+            const float f = tcx::ex2_approx(part[w][col][D] - base);
+            L = fmaf(part[w][col][D + 1], f, L);
+            O[0] = fmaf(part[w][col][d], f, O[0]);
+            O[1] = fmaf(part[w][col][d + 1], f, O[1]);
         }
-        if (a.splits > 1) {
-            float* to = a.ws + (((long long)b * a.Hq + h0 + row) * a.splits + p) * (D + 2);
-            to[d] = O;
-            if (d == 0) to[D] = M, to[D + 1] = L;
-        } else {
-            const float v = L == 0.0f ? 0.0f : O / L;
-            const long long at = b * a.os[0] + (h0 + row) * a.os[1] + d;
-            if (PAIR) static_cast<float*>(a.o)[at] = v;
-            else static_cast<__nv_bfloat16*>(a.o)[at] = __float2bfloat16_rn(v);
-            if (d == 0 && a.lse) a.lse[(long long)b * a.Hq + h0 + row] = L == 0.0f ? -INFINITY : M * kLn2 + logf(L);
-        }
+        finish(col, d, M, L, O, std::integral_constant<int, 2>{});
     }
 }
 
-// Joins the parts of a row: a warp has one.
+// Joins the parts of a row: a CTA has one, its warps every fourth part each.
+constexpr int kJoinWarps = 4;
 template <int D, bool F32>
-__global__ void __launch_bounds__(128) paged_join_kernel(const PagedArgs a)
+__global__ void __launch_bounds__(32 * kJoinWarps) paged_join_kernel(const PagedArgs a)
 {
-    const int lane = threadIdx.x & 31;
-    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
+    constexpr int E = D / 32;
+    __shared__ float tops[kJoinWarps], sums[kJoinWarps][D + 1];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const long long row = blockIdx.x;
     pdl_wait();
-    if (row >= (long long)a.B * a.Hq) return;
     const int b = (int)(row / a.Hq), h = (int)(row - (long long)b * a.Hq);
     const Cut cut = cut_of(a, b);
     const float* from = a.ws + row * a.splits * (D + 2);
-    float M = -INFINITY, L = 0.0f, O[D / 32];
-#pragma unroll
-    for (int e = 0; e < D / 32; ++e) O[e] = 0.0f;
-    for (int p = lane; p < cut.parts; p += 32) M = fmaxf(M, from[p * (D + 2) + D]);
+    float M = -INFINITY;
+    for (int p = threadIdx.x; p < cut.parts; p += 32 * kJoinWarps) M = fmaxf(M, from[p * (D + 2) + D]);
 #pragma unroll
     for (int k = 16; k >= 1; k >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, k));
+    if (lane == 0) tops[warp] = M;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kJoinWarps; ++w) M = fmaxf(M, tops[w]);
     const float base = M == -INFINITY ? 0.0f : M;
-    for (int p = 0; p < cut.parts; ++p) {
-        const float f = tcx::ex2_approx(from[p * (D + 2) + D] - base);
-        L = fmaf(from[p * (D + 2) + D + 1], f, L);
+    float L = 0.0f, O[E];
 #pragma unroll
-        for (int e = 0; e < D / 32; ++e) O[e] = fmaf(from[p * (D + 2) + lane + 32 * e], f, O[e]);
+    for (int e = 0; e < E; ++e) O[e] = 0.0f;
+#pragma unroll 4
+    for (int p = warp; p < cut.parts; p += kJoinWarps) {
+        const float* at = from + p * (D + 2);
+        const float f = tcx::ex2_approx(at[D] - base);
+        L = fmaf(at[D + 1], f, L);
+#pragma unroll
+        for (int e = 0; e < E; ++e) O[e] = fmaf(at[lane * E + e], f, O[e]);
     }
 #pragma unroll
-    for (int e = 0; e < D / 32; ++e) {
-        const float v = L == 0.0f ? 0.0f : O[e] / L;
-        const long long at = b * a.os[0] + h * a.os[1] + lane + 32 * e;
-        if (F32) static_cast<float*>(a.o)[at] = v;
-        else static_cast<__nv_bfloat16*>(a.o)[at] = __float2bfloat16_rn(v);
-    }
-    if (lane == 0 && a.lse) a.lse[row] = L == 0.0f ? -INFINITY : M * kLn2 + logf(L);
+    for (int e = 0; e < E; ++e) sums[warp][lane * E + e] = O[e];
+    if (lane == 0) sums[warp][D] = L;
+    __syncthreads();
+    if (threadIdx.x >= D) return;
+    const int d = threadIdx.x;
+    float x = 0.0f;
+    L = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kJoinWarps; ++w) x += sums[w][d], L += sums[w][D];
+    const float v = L == 0.0f ? 0.0f : x / L;
+    const long long at = b * a.os[0] + h * a.os[1] + d;
+    if (F32) static_cast<float*>(a.o)[at] = v;
+    else static_cast<__nv_bfloat16*>(a.o)[at] = __float2bfloat16_rn(v);
+    if (d == 0 && a.lse) a.lse[row] = L == 0.0f ? -INFINITY : M * kLn2 + logf(L);
 }
 
+long long units_of(const PagedArgs& a) { return (long long)a.B * a.Hk * ((a.Hq / a.Hk + 8 * kColTiles - 1) / (8 * kColTiles)); }
+// A warp for a unit where there are enough of them to fill the SMs, else a CTA of four.
+bool solo(const PagedArgs& a) { return a.splits == 1 && units_of(a) >= 16LL * a.sms; }
+
+template <int D, bool PAIR, int NR> cudaError_t launch_n(const PagedArgs& a, cudaStream_t st)
+{
+    constexpr int AHEAD = PAIR || NR > 1 ? 1 : 3;
+    const long long units = units_of(a) * a.splits;
+    const int blocks = (a.Hq / a.Hk + 8 * kColTiles - 1) / (8 * kColTiles);
+    if (solo(a))
+        return launch_dependent(paged_attention_kernel<D, PAIR, NR, 1, AHEAD>, dim3((unsigned)((units + kCtaWarps - 1) / kCtaWarps)),
+                                dim3(32 * kCtaWarps), 0, st, a, blocks);
+    return launch_dependent(paged_attention_kernel<D, PAIR, NR, kCtaWarps, AHEAD>, dim3((unsigned)units), dim3(32 * kCtaWarps), 0, st, a, blocks);
+}
 template <int D, bool PAIR> cudaError_t launch_t(const PagedArgs& a, cudaStream_t st)
 {
-    const int G = a.Hq / a.Hk, row_tiles = (G + 15) / 16;
-    const unsigned ctas = (unsigned)((long long)a.splits * a.B * a.Hk * row_tiles);
-    auto kernel = G <= 8 ? paged_attention_kernel<D, PAIR, true> : paged_attention_kernel<D, PAIR, false>;
-    const cudaError_t e = launch_dependent(kernel, dim3(ctas), dim3(32 * kWarps), 0, st, a, row_tiles);
+    const int G = a.Hq / a.Hk;
+    const cudaError_t e = G <= 8 ? launch_n<D, PAIR, 1>(a, st) : G <= 16 ? launch_n<D, PAIR, 2>(a, st) : launch_n<D, PAIR, kColTiles>(a, st);
     if (e != cudaSuccess || a.splits == 1) return e;
-    return launch_dependent(paged_join_kernel<D, PAIR>, dim3((unsigned)(((long long)a.B * a.Hq + 3) / 4)), dim3(128), 0, st, a);
+    return launch_dependent(paged_join_kernel<D, PAIR>, dim3((unsigned)((long long)a.B * a.Hq)), dim3(32 * kJoinWarps), 0, st, a);
 }
 
 }  // namespace
@@ -382,7 +479,7 @@ template <int D, bool PAIR> cudaError_t launch_t(const PagedArgs& a, cudaStream_
 // Enough parts for sixteen CTAs per SM, none below kMinPart tokens.
 int paged_splits(const PagedArgs& a)
 {
-    const long long units = (long long)a.B * a.Hk * ((a.Hq / a.Hk + 15) / 16), want = (16LL * a.sms + units - 1) / units;
+    const long long units = units_of(a), want = (16LL * a.sms + units - 1) / units;
     const long long most = ((long long)a.table_pages * a.page + kMinPart - 1) / kMinPart;
     return (int)std::max(1LL, std::min({want, most, 256LL}));
 }

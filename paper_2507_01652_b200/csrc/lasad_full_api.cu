@@ -98,6 +98,9 @@ int paged_args(lasad_ctx* ctx, const lasad_paged_params* p, bool append, bool qu
     if ((p->d != 32 && p->d != 64) || (p->page != 16 && p->page != 32 && p->page != 64 && p->page != 128) || p->B > 65535 ||
         (int64_t)p->table_pages * p->page > (1 << 30))
         return LASAD_ERR_UNSUPPORTED;
+    // (places in the pool are counted in 16 bytes and 32 bits)
+    if (!append && (p->pages * (p->k_pages_stride[0] / 16) >= 0xffffffffLL || p->pages * (p->v_pages_stride[0] / 16) >= 0xffffffffLL))
+        return LASAD_ERR_UNSUPPORTED;
     // (the units of a launch are counted in 32 bits)
     if (append ? p->N > (1 << 30) || ((int64_t)p->N / p->page + 2LL * p->B) * p->Hk + p->N > 0x7fffffffLL
                : (int64_t)p->B * p->Hq * 256 > 0x7fffffffLL)

@@ -2,8 +2,9 @@
 //
 //     o = sum_j p_j v_j ,   p_j = e^(scale q.k_j) / sum   over the tokens 0 .. pos of the sequence.
 //
-// Bound by reading the cache once, 2 d bytes a token and key head.  A warp takes steps of 16 tokens, straight from
-// memory into the fragments of two products on mma.sync.m16n8k16 (tokens are the rows of the first, channels those of
+// Bound by reading the cache once, 2 d bytes a token and key head.  A warp takes steps of 16 tokens, copied to
+// shared memory a few steps ahead (loads into registers came three steps early and were waited for all the same: 4.65
+// TB/s where that reads TODO), and from there into the fragments of two products on mma.sync.m16n8k16 (tokens are the rows of the first, channels those of
 // the second; the columns are the query heads that share the key head, 8 at a time, of which few are used, so the
 // tensor cores have time to spare and tcgen05's 128 rows would only add a way through shared memory).  e4m3 numbers are
 // exact in fp16, so keys and values enter without a rounding; the page's key scale multiplies the fp32 score.  The order
@@ -24,6 +25,7 @@
 // (M, l, O) go to memory and a second kernel joins them.
 #include "lasad_full.cuh"
 #include "lasad_tc_ptx.cuh"
+#include "lasad_tc_tma.cuh"
 
 #include <cuda_fp16.h>
 
@@ -43,6 +45,12 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma16816_new(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
 }
 // two e4m3 numbers to two fp16 ones
 __device__ __forceinline__ uint32_t f16_of(uint32_t x)
@@ -84,39 +92,34 @@ __device__ __forceinline__ Cut cut_of(const PagedArgs& a, int b)
     return c;
 }
 
-// A lane's share of 16 tokens (g = lane / 4, t = lane % 4): of tokens g and 8 + g the keys' channels t D / 4 .. , of tokens 2 t,
-// 2 t + 1, 8 + 2 t, 9 + 2 t the values' channels g D / 8 .. .
+// A step in shared memory: rows of D bytes, the 16-byte pieces of 64-byte rows turned by half the row's number, so that what
+// the lanes of a quarter warp read lies in different banks.
 template <int D> struct Step {
-    uint32_t k[2][D / 16], v[4][D / 32];
+    unsigned char k[kStep * D], v[kStep * D];
 };
-
-template <int D> __device__ __forceinline__ void load_key(uint32_t (&to)[D / 16], const unsigned char* at)
+template <int D> __device__ __forceinline__ int piece_at(int row, int piece)
 {
-    if constexpr (D == 64) {
-        const uint4 v = *reinterpret_cast<const uint4*>(at);
-        to[0] = v.x, to[1] = v.y, to[2] = v.z, to[3] = v.w;
-    } else {
-        const uint2 v = *reinterpret_cast<const uint2*>(at);
-        to[0] = v.x, to[1] = v.y;
-    }
+    return row * D + (D == 64 ? ((piece + (row >> 1)) & 3) * 16 : piece * 16);
 }
-template <int D> __device__ __forceinline__ void load_value(uint32_t (&to)[D / 32], const unsigned char* at)
+// The token that row i of a product's tile of 8 stands for (the order is free): what a lane reads of the values, tokens
+// 2 t, 2 t + 1 of 8, then meets no bank twice, and neither do two neighbouring rows of the keys.
+__device__ __forceinline__ int token_of(int i) { return i ^ ((i >> 1) & 1); }
+
+// 16 bytes to shared memory, or zeros
+__device__ __forceinline__ void copy16(void* to, const unsigned char* from, bool live)
 {
-    if constexpr (D == 64) {
-        const uint2 v = *reinterpret_cast<const uint2*>(at);
-        to[0] = v.x, to[1] = v.y;
-    } else {
-        to[0] = *reinterpret_cast<const uint32_t*>(at);
-    }
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(tcx::smem_u32(to)), "l"(from), "r"(live ? 16 : 0) : "memory");
 }
 
 // A unit is a sequence, a key head, up to 8 NR of its query heads and a part of the tokens; WARPS warps have it.  PAIR:
-// fp32 queries.  AHEAD: steps of a warp in flight beside the one it works on.
-template <int D, bool PAIR, int NR, int WARPS, int AHEAD>
+// fp32 queries.
+template <int D, bool PAIR, int NR, int WARPS>
 __global__ void __launch_bounds__(32 * kCtaWarps) paged_attention_kernel(const PagedArgs a, int col_blocks)
 {
     constexpr int KK = D / 16;                               // inner steps of q.k; words of a lane's key piece
     constexpr int MT = D / 16;                               // row tiles of O
+    constexpr int DEPTH = 256 / D;                           // steps of a warp in shared memory (8 KB)
+    extern __shared__ __align__(16) unsigned char steps_raw[];
     __shared__ float part[WARPS > 1 ? WARPS : 1][WARPS > 1 ? 8 * NR : 1][D + 2];
     const int lane = threadIdx.x & 31, warp = WARPS > 1 ? threadIdx.x >> 5 : 0, g = lane >> 2, t = lane & 3;
     const int G = a.Hq / a.Hk;
@@ -139,56 +142,53 @@ __global__ void __launch_bounds__(32 * kCtaWarps) paged_attention_kernel(const P
     const int steps = (max(hi - lo, 0) + kStep - 1) / kStep, mine = (steps - warp + WARPS - 1) / WARPS;
     const int* ids = a.block_table + (long long)b * a.table_pages;
     struct Pages {
-        int id;
+        uint32_t k, v;                                       // where the step's keys and values begin, in 16 bytes; k of no page: kNone
         float ks, vs;                                        // the scales
     };
+    constexpr uint32_t kNone = 0xffffffffu;
     auto fetch_pages = [&](int i) {                          // of steps i .. i + 31
-        Pages f{-1, 0.0f, 1.0f};
-        if (i + lane < mine) f.id = ids[(lo + ((i + lane) * WARPS + warp) * kStep) / a.page];
-        if (f.id >= a.pages) f.id = -1;
-        if (f.id >= 0) {
-            f.ks = a.kscale[(long long)f.id * a.Hk + hk];
-            f.vs = a.vscale[(long long)f.id * a.Hk + hk];
+        Pages f{kNone, 0u, 0.0f, 1.0f};
+        const int at = lo + ((i + lane) * WARPS + warp) * kStep;
+        int id = -1;
+        if (i + lane < mine) id = ids[at / a.page];
+        if (id >= 0 && id < a.pages) {
+            const int slot = at & (a.page - 1);
+            f.k = (uint32_t)((id * a.kps[0] + slot * a.kps[2]) >> 4);
+            f.v = (uint32_t)((id * a.vps[0] + slot * a.vps[2]) >> 4);
+            f.ks = a.kscale[(long long)id * a.Hk + hk];
+            f.vs = a.vscale[(long long)id * a.Hk + hk];
         }
         return f;
     };
     Pages now = fetch_pages(0), next = fetch_pages(32);
     int batch = 0;                                           // the first step of `now`
-    const unsigned char* const at_k = a.kp + hk * a.kps[1] + g * a.kps[2] + t * (D / 4);
-    const unsigned char* const at_v = a.vp + hk * a.vps[1] + 2 * t * a.vps[2] + g * (D / 8);
-    auto load = [&](Step<D>& s, int i) {
-        const int page = __shfl_sync(0xffffffffu, i - batch < 32 ? now.id : next.id, i & 31);
-        const int at = lo + (i * WARPS + warp) * kStep, slot = at & (a.page - 1);
-        const int live = page >= 0 && i < mine ? hi - at : 0;        // tokens of the step that count
-        const unsigned char* k = at_k + page * a.kps[0] + slot * a.kps[2];
-        const unsigned char* v = at_v + page * a.vps[0] + slot * a.vps[2];
-        if (live >= kStep) {
-            load_key<D>(s.k[0], k);
-            load_key<D>(s.k[1], k + 8 * a.kps[2]);
-            load_value<D>(s.v[0], v);
-            load_value<D>(s.v[1], v + a.vps[2]);
-            load_value<D>(s.v[2], v + 8 * a.vps[2]);
-            load_value<D>(s.v[3], v + 9 * a.vps[2]);
-        } else {
+    // A lane copies pieces of 16 bytes: of keys and values 32 at a time, rows row0, row0 + ROWS ..
+    constexpr int PIECES = D / 16, ROWS = 32 / PIECES;
+    Step<D>* const ring = reinterpret_cast<Step<D>*>(steps_raw) + (threadIdx.x >> 5) * DEPTH;
+    const int row0 = lane / PIECES, piece = lane % PIECES;
+    const unsigned char* const at_k = a.kp + hk * a.kps[1] + row0 * a.kps[2] + piece * 16;
+    const unsigned char* const at_v = a.vp + hk * a.vps[1] + row0 * a.vps[2] + piece * 16;
+    const long long next_k = ROWS * a.kps[2], next_v = ROWS * a.vps[2];
+    auto load = [&](int i) {
+        const uint32_t from_k = __shfl_sync(0xffffffffu, i - batch < 32 ? now.k : next.k, i & 31);
+        const uint32_t from_v = __shfl_sync(0xffffffffu, i - batch < 32 ? now.v : next.v, i & 31);
+        if (i < mine) {
             // (what does not count is 0, whatever stands there: a weight of 0 times a NaN is not 0)
+            const int live = from_k != kNone ? hi - (lo + (i * WARPS + warp) * kStep) : 0;
+            const unsigned char* k = at_k + (live > 0 ? from_k : 0) * 16ull;
+            const unsigned char* v = at_v + (live > 0 ? from_v : 0) * 16ull;
+            Step<D>& s = ring[i & (DEPTH - 1)];
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
-#pragma unroll
-                for (int e = 0; e < D / 16; ++e) s.k[n][e] = 0u;
-                if (8 * n + g < live) load_key<D>(s.k[n], k + 8 * n * a.kps[2]);
-            }
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                const int token = (n & 1) + 8 * (n >> 1);
-#pragma unroll
-                for (int e = 0; e < D / 32; ++e) s.v[n][e] = 0u;
-                if (2 * t + token < live) load_value<D>(s.v[n], v + token * a.vps[2]);
+            for (int n = 0; n < kStep / ROWS; ++n) {
+                const int row = row0 + n * ROWS;
+                copy16(s.k + piece_at<D>(row, piece), k + n * next_k, row < live);
+                copy16(s.v + piece_at<D>(row, piece), v + n * next_v, row < live);
             }
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    Step<D> ring[AHEAD + 1];
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) load(ring[i], i);
+    for (int i = 0; i < DEPTH - 1; ++i) load(i);
 
     // q as fp16 fragments: inner step kk, register r: column g (query head), channels t D / 4 + 4 kk + 2 r and the next
     uint32_t qb[NR][KK][2], ql[PAIR ? NR : 1][PAIR ? KK : 1][2];
@@ -234,13 +234,13 @@ __global__ void __launch_bounds__(32 * kCtaWarps) paged_attention_kernel(const P
             }
     }
     // scores have columns 2 t and 2 t + 1 (i) in a lane
-    float factor[NR][2], m[NR][2], l[NR][2], o[NR][MT][4];
+    float factor[NR][2], M[NR][2], l[NR][2], o[NR][MT][4];   // (M is -infinity until a row has seen something)
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             factor[n][i] = __shfl_sync(0xffffffffu, mine_factor[n], 4 * (2 * t + i));
-            m[n][i] = -INFINITY;
+            M[n][i] = -INFINITY;
             l[n][i] = 0.0f;
         }
 #pragma unroll
@@ -248,59 +248,90 @@ __global__ void __launch_bounds__(32 * kCtaWarps) paged_attention_kernel(const P
     }
 
     float lv = log2f(now.vs), iv = 1.0f / now.vs;            // of the value scales: log2 and reciprocal
-    auto work = [&](const Step<D>& s, int i) {
+    auto live_of = [&](int i) { return now.k == kNone ? 0 : hi - (lo + ((i + lane) * WARPS + warp) * kStep); };
+    int lives = live_of(0);                                  // tokens that count
+    // a lane's places in a step: keys of tokens g and 8 + g, values of tokens 2 t, 2 t + 1 and 8 further
+    const int at_key = D == 64 ? piece_at<D>(token_of(g), t) : token_of(g) * D + t * 8;
+    const int at_value0 = D == 64 ? piece_at<D>(token_of(2 * t), g >> 1) + (g & 1) * 8 : token_of(2 * t) * D + g * 4;
+    const int at_value1 = D == 64 ? piece_at<D>(token_of(2 * t + 1), g >> 1) + (g & 1) * 8 : token_of(2 * t + 1) * D + g * 4;
+    auto work = [&](int i) {
+        struct {
+            uint32_t k[2][D / 16], v[4][D / 32];
+        } s;
+        const Step<D>& from = ring[i & (DEPTH - 1)];
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            if constexpr (D == 64) {
+                const uint4 x = *reinterpret_cast<const uint4*>(from.k + at_key + 8 * n * D);
+                s.k[n][0] = x.x, s.k[n][1] = x.y, s.k[n][2] = x.z, s.k[n][3] = x.w;
+                const uint2 y = *reinterpret_cast<const uint2*>(from.v + at_value0 + 8 * n * D);
+                const uint2 z = *reinterpret_cast<const uint2*>(from.v + at_value1 + 8 * n * D);
+                s.v[2 * n][0] = y.x, s.v[2 * n][1] = y.y, s.v[2 * n + 1][0] = z.x, s.v[2 * n + 1][1] = z.y;
+            } else {
+                const uint2 x = *reinterpret_cast<const uint2*>(from.k + at_key + 8 * n * D);
+                s.k[n][0] = x.x, s.k[n][1] = x.y;
+                s.v[2 * n][0] = *reinterpret_cast<const uint32_t*>(from.v + at_value0 + 8 * n * D);
+                s.v[2 * n + 1][0] = *reinterpret_cast<const uint32_t*>(from.v + at_value1 + 8 * n * D);
+            }
+        }
         const float step_ks = __shfl_sync(0xffffffffu, now.ks, i & 31), step_lv = __shfl_sync(0xffffffffu, lv, i & 31);
         const float step_iv = __shfl_sync(0xffffffffu, iv, i & 31);
-        const int page = __shfl_sync(0xffffffffu, now.id, i & 31), live = page < 0 ? 0 : hi - (lo + (i * WARPS + warp) * kStep);
+        const int step_live = __shfl_sync(0xffffffffu, lives, i & 31);
         // scores: c[0..1] of token g, c[2..3] of token 8 + g
         float c[NR][4];
-#pragma unroll
-        for (int n = 0; n < NR; ++n) c[n][0] = c[n][1] = c[n][2] = c[n][3] = 0.0f;
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
             const uint32_t f[4] = {f16_of(s.k[0][kk]), f16_of(s.k[1][kk]), f16_of(s.k[0][kk] >> 16), f16_of(s.k[1][kk] >> 16)};
 #pragma unroll
             for (int n = 0; n < NR; ++n) {
-                mma16816(c[n], f, qb[n][kk][0], qb[n][kk][1]);
+                if (kk == 0) mma16816_new(c[n], f, qb[n][kk][0], qb[n][kk][1]);
+                else mma16816(c[n], f, qb[n][kk][0], qb[n][kk][1]);
                 if (PAIR) mma16816(c[n], f, ql[n][kk][0], ql[n][kk][1]);
             }
         }
+        // c becomes x - M; over kLift + kLag somewhere, M moves
         bool grow = false;
 #pragma unroll
         for (int n = 0; n < NR; ++n)
 #pragma unroll
-            for (int i2 = 0; i2 < 2; ++i2) {
-                const float f = step_ks * factor[n][i2];
-                c[n][i2] = fmaf(c[n][i2], f, step_lv);
-                c[n][2 + i2] = fmaf(c[n][2 + i2], f, step_lv);
-                if (live < kStep) {
-                    if (g >= live) c[n][i2] = -INFINITY;
-                    if (8 + g >= live) c[n][2 + i2] = -INFINITY;
-                }
-                grow = grow || fmaxf(c[n][i2], c[n][2 + i2]) > m[n][i2] + (kLift + kLag);
+            for (int e = 0; e < 2; ++e) {
+                const float f = step_ks * factor[n][e], base = step_lv - (M[n][e] == -INFINITY ? 0.0f : M[n][e]);
+                c[n][e] = fmaf(c[n][e], f, base);
+                c[n][2 + e] = fmaf(c[n][2 + e], f, base);
+                grow = grow || M[n][e] == -INFINITY || fmaxf(c[n][e], c[n][2 + e]) > kLift + kLag;
             }
+        if (step_live < kStep) {
+#pragma unroll
+            for (int n = 0; n < NR; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (token_of(g) + 8 * (e >> 1) >= step_live) c[n][e] = -INFINITY;
+        }
         if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
             for (int n = 0; n < NR; ++n)
 #pragma unroll
-                for (int i2 = 0; i2 < 2; ++i2) {
-                    float top = fmaxf(c[n][i2], c[n][2 + i2]);
+                for (int e = 0; e < 2; ++e) {
+                    float top = fmaxf(c[n][e], c[n][2 + e]);
 #pragma unroll
                     for (int k = 4; k <= 16; k <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
-                    const float now = fmaxf(m[n][i2], top - kLift), f = now == m[n][i2] ? 1.0f : tcx::ex2_approx(m[n][i2] - now);
-                    m[n][i2] = now;
-                    l[n][i2] *= f;
+                    // (top is over M, or over 0 where there is none yet)
+                    const float old = M[n][e], was = old == -INFINITY ? 0.0f : old;
+                    if (top == -INFINITY || (old != -INFINITY && top <= kLift)) continue;
+                    M[n][e] = was + (top - kLift);
+                    const float f = old == -INFINITY ? 0.0f : tcx::ex2_approx(old - M[n][e]);
+                    c[n][e] -= M[n][e] - was, c[n][2 + e] -= M[n][e] - was;
+                    l[n][e] *= f;
 #pragma unroll
-                    for (int k = 0; k < MT; ++k) o[n][k][i2] *= f, o[n][k][2 + i2] *= f;
+                    for (int k = 0; k < MT; ++k) o[n][k][e] *= f, o[n][k][2 + e] *= f;
                 }
         }
         uint32_t w[NR][2], wl[PAIR ? NR : 1][2];
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
-            const float b0 = m[n][0] == -INFINITY ? 0.0f : m[n][0], b1 = m[n][1] == -INFINITY ? 0.0f : m[n][1];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const float x0 = tcx::ex2_approx(c[n][2 * k] - b0), x1 = tcx::ex2_approx(c[n][2 * k + 1] - b1);
+                const float x0 = tcx::ex2_approx(c[n][2 * k]), x1 = tcx::ex2_approx(c[n][2 * k + 1]);
                 l[n][0] = fmaf(x0, step_iv, l[n][0]);
                 l[n][1] = fmaf(x1, step_iv, l[n][1]);
                 const uint32_t packed = pack_f16(x0, x1);
@@ -323,19 +354,17 @@ __global__ void __launch_bounds__(32 * kCtaWarps) paged_attention_kernel(const P
                 }
             }
     };
-    for (int i = 0; i < mine; i += AHEAD + 1) {
+    for (int i = 0; i < mine; ++i) {
         if (i - batch == 32) {
             now = next;
             batch = i;
-            lv = log2f(now.vs), iv = 1.0f / now.vs;
+            lv = log2f(now.vs), iv = 1.0f / now.vs, lives = live_of(i);
             next = fetch_pages(i + 32);
         }
-#pragma unroll
-        for (int k = 0; k <= AHEAD; ++k) {
-            if (i + k >= mine) break;
-            load(ring[(k + AHEAD) % (AHEAD + 1)], i + k + AHEAD);
-            work(ring[k], i + k);
-        }
+        asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 2) : "memory");
+        __syncwarp();                                        // (step i is there, and step i - 1 has been read by all lanes)
+        load(i + DEPTH - 1);
+        work(i);
     }
 #pragma unroll
     for (int n = 0; n < NR; ++n)
@@ -374,12 +403,12 @@ __global__ void __launch_bounds__(32 * kCtaWarps) paged_attention_kernel(const P
             for (int k = 0; k < MT; ++k) x[2 * k] = o[n][k][i], x[2 * k + 1] = o[n][k][2 + i];
             const int col = 8 * n + 2 * t + i;
             if (WARPS == 1) {
-                if (col < heads) finish(col, g * (D / 8), m[n][i], l[n][i], x, std::integral_constant<int, D / 8>{});
+                if (col < heads) finish(col, g * (D / 8), M[n][i], l[n][i], x, std::integral_constant<int, D / 8>{});
             } else {
                 float* to = part[warp][col];
 #pragma unroll
                 for (int e = 0; e < D / 8; e += 2) *reinterpret_cast<float2*>(to + g * (D / 8) + e) = make_float2(x[e], x[e + 1]);
-                if (g == 0) *reinterpret_cast<float2*>(to + D) = make_float2(m[n][i], l[n][i]);
+                if (g == 0) *reinterpret_cast<float2*>(to + D) = make_float2(M[n][i], l[n][i]);
             }
         }
     if (WARPS == 1) return;
@@ -458,13 +487,17 @@ bool solo(const PagedArgs& a) { return a.splits == 1 && units_of(a) >= 16LL * a.
 
 template <int D, bool PAIR, int NR> cudaError_t launch_n(const PagedArgs& a, cudaStream_t st)
 {
-    constexpr int AHEAD = PAIR || NR > 1 ? 1 : 3;
+    constexpr size_t smem = (size_t)kCtaWarps * (256 / D) * sizeof(Step<D>);
     const long long units = units_of(a) * a.splits;
     const int blocks = (a.Hq / a.Hk + 8 * kColTiles - 1) / (8 * kColTiles);
+    static bool done1[64], done2[64];
+    cudaError_t e = tcx::allow_dynamic_smem(paged_attention_kernel<D, PAIR, NR, 1>, smem, done1);
+    if (e == cudaSuccess) e = tcx::allow_dynamic_smem(paged_attention_kernel<D, PAIR, NR, kCtaWarps>, smem, done2);
+    if (e != cudaSuccess) return e;
     if (solo(a))
-        return launch_dependent(paged_attention_kernel<D, PAIR, NR, 1, AHEAD>, dim3((unsigned)((units + kCtaWarps - 1) / kCtaWarps)),
-                                dim3(32 * kCtaWarps), 0, st, a, blocks);
-    return launch_dependent(paged_attention_kernel<D, PAIR, NR, kCtaWarps, AHEAD>, dim3((unsigned)units), dim3(32 * kCtaWarps), 0, st, a, blocks);
+        return launch_dependent(paged_attention_kernel<D, PAIR, NR, 1>, dim3((unsigned)((units + kCtaWarps - 1) / kCtaWarps)),
+                                dim3(32 * kCtaWarps), smem, st, a, blocks);
+    return launch_dependent(paged_attention_kernel<D, PAIR, NR, kCtaWarps>, dim3((unsigned)units), dim3(32 * kCtaWarps), smem, st, a, blocks);
 }
 template <int D, bool PAIR> cudaError_t launch_t(const PagedArgs& a, cudaStream_t st)
 {

@@ -120,7 +120,8 @@ __global__ void __launch_bounds__(32 * kCtaWarps) paged_attention_kernel(const P
     constexpr int MT = D / 16;                               // row tiles of O
     constexpr int DEPTH = 256 / D;                           // steps of a warp in shared memory (8 KB)
     extern __shared__ __align__(16) unsigned char steps_raw[];
-    __shared__ float part[WARPS > 1 ? WARPS : 1][WARPS > 1 ? 8 * NR : 1][D + 2];
+    static_assert(8 * NR * (D + 2) * 4 <= DEPTH * sizeof(Step<D>), "a warp's part of the result takes the place of its steps");
+    auto part = reinterpret_cast<float (*)[8 * NR][D + 2]>(steps_raw);
     const int lane = threadIdx.x & 31, warp = WARPS > 1 ? threadIdx.x >> 5 : 0, g = lane >> 2, t = lane & 3;
     const int G = a.Hq / a.Hk;
     // unit = ((part * B + sequence) * Hk + key head) * col_blocks + block of query heads
@@ -394,6 +395,7 @@ __global__ void __launch_bounds__(32 * kCtaWarps) paged_attention_kernel(const P
         }
         if (d == 0 && a.lse) a.lse[(long long)b * a.Hq + h] = L == 0.0f ? -INFINITY : M * kLn2 + logf(L);
     };
+    if (WARPS > 1) __syncthreads();                          // (their steps have been read)
 #pragma unroll
     for (int n = 0; n < NR; ++n)
 #pragma unroll
@@ -431,54 +433,76 @@ __global__ void __launch_bounds__(32 * kCtaWarps) paged_attention_kernel(const P
     }
 }
 
-// Joins the parts of a row: a CTA has one, its warps every fourth part each.
-constexpr int kJoinWarps = 4;
+// Joins the parts of a row: a CTA has one, its warps every eighth part each.  The first kBatch of a warp's are asked for
+// before it is known how many there are (what stands in the others is not used).
+constexpr int kJoinWarps = 8, kBatch = 4;
 template <int D, bool F32>
 __global__ void __launch_bounds__(32 * kJoinWarps) paged_join_kernel(const PagedArgs a)
 {
     constexpr int E = D / 32;
     __shared__ float tops[kJoinWarps], sums[kJoinWarps][D + 1];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const long long row = blockIdx.x;
-    pdl_wait();
-    const int b = (int)(row / a.Hq), h = (int)(row - (long long)b * a.Hq);
-    const Cut cut = cut_of(a, b);
-    const float* from = a.ws + row * a.splits * (D + 2);
-    float M = -INFINITY;
-    for (int p = threadIdx.x; p < cut.parts; p += 32 * kJoinWarps) M = fmaxf(M, from[p * (D + 2) + D]);
-#pragma unroll
-    for (int k = 16; k >= 1; k >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, k));
-    if (lane == 0) tops[warp] = M;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kJoinWarps; ++w) M = fmaxf(M, tops[w]);
-    const float base = M == -INFINITY ? 0.0f : M;
-    float L = 0.0f, O[E];
+    const int b = blockIdx.x / a.Hq, h = blockIdx.x - b * a.Hq;
+    const float* from = a.ws + (long long)blockIdx.x * a.splits * (D + 2);
+    float M = -INFINITY, L = 0.0f, O[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) O[e] = 0.0f;
-#pragma unroll 4
-    for (int p = warp; p < cut.parts; p += kJoinWarps) {
-        const float* at = from + p * (D + 2);
-        const float f = tcx::ex2_approx(at[D] - base);
-        L = fmaf(at[D + 1], f, L);
+    pdl_wait();
+    int parts = a.splits;
+    for (int p0 = warp; p0 < parts; p0 += kJoinWarps * kBatch) {
+        float m[kBatch], l[kBatch], o[kBatch][E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) O[e] = fmaf(at[lane * E + e], f, O[e]);
+        for (int k = 0; k < kBatch; ++k) {
+            const float* at = from + min(p0 + k * kJoinWarps, a.splits - 1) * (D + 2);
+            const float2 ml = *reinterpret_cast<const float2*>(at + D);
+            m[k] = ml.x, l[k] = ml.y;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[k][e] = at[lane * E + e];
+        }
+        if (p0 == warp) parts = cut_of(a, b).parts;
+        float top = M;
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            if (p0 + k * kJoinWarps >= parts) m[k] = -INFINITY, l[k] = 0.0f;
+            top = fmaxf(top, m[k]);
+        }
+        if (top == -INFINITY) continue;
+        const float f0 = tcx::ex2_approx(M - top);
+        M = top;
+        L *= f0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) O[e] *= f0;
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            if (m[k] == -INFINITY) continue;
+            const float f = tcx::ex2_approx(m[k] - M);
+            L = fmaf(l[k], f, L);
+#pragma unroll
+            for (int e = 0; e < E; ++e) O[e] = fmaf(o[k][e], f, O[e]);
+        }
     }
+    if (lane == 0) tops[warp] = M, sums[warp][D] = L;
 #pragma unroll
     for (int e = 0; e < E; ++e) sums[warp][lane * E + e] = O[e];
-    if (lane == 0) sums[warp][D] = L;
     __syncthreads();
     if (threadIdx.x >= D) return;
     const int d = threadIdx.x;
+    M = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kJoinWarps; ++w) M = fmaxf(M, tops[w]);
+    const float base = M == -INFINITY ? 0.0f : M;
     float x = 0.0f;
     L = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kJoinWarps; ++w) x += sums[w][d], L += sums[w][D];
+    for (int w = 0; w < kJoinWarps; ++w) {
+        const float f = tcx::ex2_approx(tops[w] - base);
+        x = fmaf(sums[w][d], f, x), L = fmaf(sums[w][D], f, L);
+    }
     const float v = L == 0.0f ? 0.0f : x / L;
     const long long at = b * a.os[0] + h * a.os[1] + d;
     if (F32) static_cast<float*>(a.o)[at] = v;
     else static_cast<__nv_bfloat16*>(a.o)[at] = __float2bfloat16_rn(v);
-    if (d == 0 && a.lse) a.lse[row] = L == 0.0f ? -INFINITY : M * kLn2 + logf(L);
+    if (d == 0 && a.lse) a.lse[blockIdx.x] = L == 0.0f ? -INFINITY : M * kLn2 + logf(L);
 }
 
 long long units_of(const PagedArgs& a) { return (long long)a.B * a.Hk * ((a.Hq / a.Hk + 8 * kColTiles - 1) / (8 * kColTiles)); }
@@ -509,12 +533,13 @@ template <int D, bool PAIR> cudaError_t launch_t(const PagedArgs& a, cudaStream_
 
 }  // namespace
 
-// Enough parts for sixteen CTAs per SM, none below kMinPart tokens.
+// Enough parts for sixteen CTAs per SM, none below kMinPart tokens; a short table is not cut (a second launch costs what a
+// CTA does in four parts' time).
 int paged_splits(const PagedArgs& a)
 {
-    const long long units = units_of(a), want = (16LL * a.sms + units - 1) / units;
-    const long long most = ((long long)a.table_pages * a.page + kMinPart - 1) / kMinPart;
-    return (int)std::max(1LL, std::min({want, most, 256LL}));
+    const long long units = units_of(a), tokens = (long long)a.table_pages * a.page, want = (16LL * a.sms + units - 1) / units;
+    if (tokens <= 4 * kMinPart) return 1;
+    return (int)std::max(1LL, std::min({want, (tokens + kMinPart - 1) / kMinPart, 256LL}));
 }
 
 size_t paged_workspace_bytes(const PagedArgs& a)

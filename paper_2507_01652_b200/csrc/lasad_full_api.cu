@@ -102,7 +102,7 @@ int paged_args(lasad_ctx* ctx, const lasad_paged_params* p, bool append, bool qu
     if (!append && (p->pages * (p->k_pages_stride[0] / 16) >= 0xffffffffLL || p->pages * (p->v_pages_stride[0] / 16) >= 0xffffffffLL))
         return LASAD_ERR_UNSUPPORTED;
     // (the units of a launch are counted in 32 bits)
-    if (append ? p->N > (1 << 30) || ((int64_t)p->N / p->page + 2LL * p->B) * p->Hk + p->N > 0x7fffffffLL
+    if (append ? p->N > (1 << 30) || 2 * ((int64_t)p->N / p->page + 2LL * p->B) * p->Hk + (int64_t)p->N * p->Hq > 0x7fffffffLL
                : (int64_t)p->B * p->Hq * 256 > 0x7fffffffLL)
         return LASAD_ERR_UNSUPPORTED;
     if (!on_device(ctx)) return LASAD_ERR_INVALID_ARG;

@@ -56,33 +56,46 @@ __device__ __forceinline__ float2 from_e4m3(uint32_t x)
 }
 
 // Channels of lane `sub` of a row's D / 8 lanes: with HALF sub * 4 .. + 3 and their partners D / 2 further, else
-// sub * 8 .. + 7; x[0..3] are the pairs' first channels, x[4..7] their partners.
-template <typename T, int D, bool HALF> __device__ __forceinline__ void load_pairs(const T* row, int sub, float (&x)[8])
-{
-    using namespace tcx;
-    if constexpr (sizeof(T) == 2) {
-        uint32_t w[4];
+// sub * 8 .. + 7; as they come from memory, and in get() as the pairs' first channels x[0..3] and their partners x[4..7].
+template <typename T, int D, bool HALF> struct Piece;
+template <int D, bool HALF> struct Piece<__nv_bfloat16, D, HALF> {
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const __nv_bfloat16* row, int sub)
+    {
         if (HALF) {
             const uint2 a = *reinterpret_cast<const uint2*>(row + sub * 4), b = *reinterpret_cast<const uint2*>(row + D / 2 + sub * 4);
             w[0] = a.x, w[1] = a.y, w[2] = b.x, w[3] = b.y;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[2 * i] = bf16_lo(w[i]), x[2 * i + 1] = bf16_hi(w[i]);
         } else {
             const uint4 a = *reinterpret_cast<const uint4*>(row + sub * 8);
             w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = bf16_lo(w[i]), x[4 + i] = bf16_hi(w[i]);
         }
-    } else {
-        const float4 a = *reinterpret_cast<const float4*>(row + (HALF ? sub * 4 : sub * 8));
-        const float4 b = *reinterpret_cast<const float4*>(row + (HALF ? D / 2 + sub * 4 : sub * 8 + 4));
+    }
+    __device__ __forceinline__ void get(float (&x)[8]) const
+    {
+        using namespace tcx;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (HALF) x[2 * i] = bf16_lo(w[i]), x[2 * i + 1] = bf16_hi(w[i]);
+            else x[i] = bf16_lo(w[i]), x[4 + i] = bf16_hi(w[i]);
+        }
+    }
+};
+template <int D, bool HALF> struct Piece<float, D, HALF> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float* row, int sub)
+    {
+        a = *reinterpret_cast<const float4*>(row + (HALF ? sub * 4 : sub * 8));
+        b = *reinterpret_cast<const float4*>(row + (HALF ? D / 2 + sub * 4 : sub * 8 + 4));
+    }
+    __device__ __forceinline__ void get(float (&x)[8]) const
+    {
         if (HALF) {
             x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
         } else {
             x[0] = a.x, x[4] = a.y, x[1] = a.z, x[5] = a.w, x[2] = b.x, x[6] = b.y, x[3] = b.z, x[7] = b.w;
         }
     }
-}
+};
 template <typename T, int D, bool HALF> __device__ __forceinline__ void store_pairs(T* row, int sub, const float (&x)[8])
 {
     using namespace tcx;
@@ -153,18 +166,22 @@ __device__ __forceinline__ Fresh fresh_of(const PagedArgs& a, int b)
     return f;
 }
 
-// One page and head: `page` / kStep warps, kStep tokens each; first keys, then values.
+// A page's keys or values of some heads: `page` / kStep warps (a team), kStep tokens each; head after head, the next one's
+// rows on their way while one is worked on.
 template <typename T, int D, bool HALF, bool TURN>
-__device__ __forceinline__ void write_page(const PagedArgs& a, int unit, float (&top)[2][kWarps])
+__device__ __forceinline__ void write_page(const PagedArgs& a, int cta, int numbers, int per, int groups, float (&tops)[2][kWarps])
 {
     constexpr int LANES = D / 8, ROWS = 32 / LANES, ACC = kStep / ROWS;     // lanes of a row, rows of an access, accesses
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane % LANES, mine = lane / LANES;
     const int W = a.page / kStep, team = warp / W, w = warp - team * W;     // a page's warps
-    unit = unit * (kWarps / W) + team;
-    const int at = unit / a.Hk, h = unit - at * a.Hk;
+    // unit = (page number * groups + group of heads) * 2 + values
+    int unit = cta * (kWarps / W) + team;
+    const int kv = unit & 1;
+    unit >>= 1;
+    const int at = unit / groups, h0 = (unit - at * groups) * per, h1 = min(h0 + per, a.Hk);
+    if (at >= numbers) return;
     // the page: of sequence b its page number j (see region_tiles for numbers without a table)
     int b = at, j = 0;
-    bool live;
     if (a.offsets) {
         int lo = 0, hi = a.B;
         while (hi - lo > 1) {
@@ -174,36 +191,50 @@ __device__ __forceinline__ void write_page(const PagedArgs& a, int unit, float (
         }
         b = lo;
         j = at - (max(0, min(a.offsets[b], a.N)) / a.page + 2 * b);
-        live = j >= 0;
-    } else {
-        live = b < a.B;
+        if (j < 0) return;
     }
-    Fresh f{0, 0, 0};
-    if (live) f = fresh_of(a, b);
-    live = live && f.pos >= 0 && f.n > 0;
-    const long long page0 = live ? (f.pos / a.page + j) * a.page : 0;       // the position of the page's first slot
-    live = live && page0 < f.pos + f.n && page0 / a.page < a.table_pages;
-    int id = -1;
-    if (live) id = a.block_table[(long long)b * a.table_pages + page0 / a.page];
-    live = live && id >= 0 && id < a.pages;
-    // slots first .. last - 1 are new
-    const int first = live ? (int)max(0LL, f.pos - page0) : 0, last = live ? (int)min((long long)a.page, f.pos + f.n - page0) : 0;
-    const long long row0 = f.at + (page0 - f.pos);                          // the row of the page's slot 0
-    for (int kv = 0; kv < 2; ++kv) {
-        const T* src = static_cast<const T*>(kv ? a.v : a.k) + h * (kv ? a.vs[1] : a.ks[1]);
-        const long long stride = kv ? a.vs[0] : a.ks[0];
+    const Fresh f = fresh_of(a, b);
+    if (f.pos < 0 || f.n <= 0) return;
+    const long long page0 = (f.pos / a.page + j) * a.page;                  // the position of the page's first slot
+    if (page0 >= f.pos + f.n || page0 / a.page >= a.table_pages) return;
+    const int id = a.block_table[(long long)b * a.table_pages + page0 / a.page];
+    if (id < 0 || id >= a.pages) return;
+    // slots first .. last - 1 are new; the row of slot 0
+    const int first = (int)max(0LL, f.pos - page0), last = (int)min((long long)a.page, f.pos + f.n - page0);
+    const long long row0 = f.at + (page0 - f.pos), stride = kv ? a.vs[0] : a.ks[0], next_head = kv ? a.vs[1] : a.ks[1];
+    const T* src = static_cast<const T*>(kv ? a.v : a.k) + (row0 + w * kStep + mine) * stride;
+    const long long slots = kv ? a.vps[2] : a.kps[2];
+    auto fresh = [&](int i) {
+        const int slot = w * kStep + i * ROWS + mine;
+        return slot >= first && slot < last;
+    };
+    auto fetch = [&](Piece<T, D, HALF> (&to)[ACC], int h) {
+#pragma unroll
+        for (int i = 0; i < ACC; ++i)
+            if (fresh(i)) to[i].load(src + i * ROWS * stride + h * next_head, sub);
+    };
+    Piece<T, D, HALF> now[ACC];
+    fetch(now, h0);
+    float c[ACC][4], s[ACC][4];
+    if (TURN && kv == 0) {
+#pragma unroll
+        for (int i = 0; i < ACC; ++i) angles<D>(a, page0 + w * kStep + i * ROWS + mine, sub, c[i], s[i]);
+    }
+    for (int h = h0; h < h1; ++h) {
+        float* scale = (kv ? a.vscale : a.kscale) + (long long)id * a.Hk + h;
+        unsigned char* dst = kv ? a.vp + id * a.vps[0] + h * a.vps[1] : a.kp + id * a.kps[0] + h * a.kps[1];
+        const float was = first > 0 ? *scale : 0.0f;
+        Piece<T, D, HALF> next[ACC];
+        if (h + 1 < h1) fetch(next, h + 1);
         float x[ACC][8], size = 0.0f;
 #pragma unroll
         for (int i = 0; i < ACC; ++i) {
-            const int slot = w * kStep + i * ROWS + mine;
-            if (slot < first || slot >= last) continue;
-            load_pairs<T, D, HALF>(src + (row0 + slot) * stride, sub, x[i]);
+            if (!fresh(i)) continue;
+            now[i].get(x[i]);
             if (TURN && kv == 0) {
-                float c[4], s[4];
-                angles<D>(a, page0 + slot, sub, c, s);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const double x0 = x[i][e], x1 = x[i][4 + e], cd = c[e], sd = s[e];
+                    const double x0 = x[i][e], x1 = x[i][4 + e], cd = c[i][e], sd = s[i][e];
                     x[i][e] = (float)(x0 * cd - x1 * sd);
                     x[i][4 + e] = (float)(x0 * sd + x1 * cd);
                 }
@@ -213,22 +244,19 @@ __device__ __forceinline__ void write_page(const PagedArgs& a, int unit, float (
         }
 #pragma unroll
         for (int k = 16; k >= 1; k >>= 1) size = fmaxf(size, __shfl_xor_sync(0xffffffffu, size, k));
-        if (lane == 0) top[kv][warp] = size;
-        __syncthreads();
-        for (int k = 0; k < W; ++k) size = fmaxf(size, top[kv][team * W + k]);
-        float* scale = (kv ? a.vscale : a.kscale) + (long long)id * a.Hk + h;
-        unsigned char* dst = kv ? a.vp + id * a.vps[0] + h * a.vps[1] : a.kp + id * a.kps[0] + h * a.kps[1];
-        const long long slots = kv ? a.vps[2] : a.kps[2];
-        float now = power_of_two(scale_exponent(size)), was = now;
-        if (live && first > 0) {
-            was = *scale;
-            now = fmaxf(now, was);
+        if (W > 1) {
+            // (two places in turn: who is a head ahead has met the others since they read this one's)
+            float (&top)[kWarps] = tops[h & 1];
+            if (lane == 0) top[warp] = size;
+            asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + team), "r"(32 * W) : "memory");
+            for (int k = 0; k < W; ++k) size = fmaxf(size, top[team * W + k]);
+        } else {
+            __syncwarp();                                                   // (everyone has read the scale)
         }
-        __syncthreads();                                                    // (everyone has read the scale)
-        if (!live) continue;
-        if (w == 0 && lane == 0) *scale = now;
-        if (now > was) {
-            const float f8 = was / now;
+        const float now_s = fmaxf(power_of_two(scale_exponent(size)), was);
+        if (w == 0 && lane == 0) *scale = now_s;
+        if (first > 0 && now_s > was) {
+            const float f8 = was / now_s;
             for (int slot = w * ROWS + mine; slot < first; slot += W * ROWS) {
                 unsigned char* row = dst + slot * slots + sub * 8;
                 uint2 old = *reinterpret_cast<const uint2*>(row);
@@ -241,22 +269,24 @@ __device__ __forceinline__ void write_page(const PagedArgs& a, int unit, float (
                 *reinterpret_cast<uint2*>(row) = make_uint2(r[0], r[1]);
             }
         }
-        const float inv = 1.0f / now;
+        const float inv = 1.0f / now_s;
 #pragma unroll
         for (int i = 0; i < ACC; ++i) {
-            const int slot = w * kStep + i * ROWS + mine;
-            if (slot >= first && slot < last) store_bytes<D, HALF>(dst + slot * slots, sub, x[i], inv);
+            if (fresh(i)) store_bytes<D, HALF>(dst + (w * kStep + i * ROWS + mine) * slots, sub, x[i], inv);
+            now[i] = next[i];
         }
     }
 }
 
-// A row of lanes has a token; it goes over the query heads.
+// A row of lanes has a token and some of its query heads, kTogether at a time.
+constexpr int kTogether = 4;
 template <typename T, int D, bool HALF, bool TURN>
-__device__ __forceinline__ void turn_queries(const PagedArgs& a, int cta)
+__device__ __forceinline__ void turn_queries(const PagedArgs& a, int cta, int per, int groups)
 {
     constexpr int LANES = D / 8, ROWS = 32 / LANES;
     const int sub = threadIdx.x % LANES;
-    const long long row = (long long)cta * kWarps * ROWS + threadIdx.x / LANES;
+    const int group = cta % groups, h0 = group * per, h1 = min(h0 + per, a.Hq);
+    const long long row = (long long)(cta / groups) * kWarps * ROWS + threadIdx.x / LANES;
     if (row >= a.N) return;
     // its sequence and position
     int b = (int)row;
@@ -282,38 +312,64 @@ __device__ __forceinline__ void turn_queries(const PagedArgs& a, int cta)
     if (TURN && live) angles<D>(a, pos, sub, c, s);
     const T* src = static_cast<const T*>(a.q) + row * a.qs[0];
     T* dst = static_cast<T*>(a.q_out) + row * a.qos[0];
-    for (int h = 0; h < a.Hq; ++h) {
-        float x[8], y[8];
-        load_pairs<T, D, HALF>(src + h * a.qs[1], sub, x);
+    for (int h = h0; h < h1; h += kTogether) {
+        Piece<T, D, HALF> piece[kTogether];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            y[e] = live ? TURN ? x[e] * c[e] - x[4 + e] * s[e] : x[e] : 0.0f;
-            y[4 + e] = live ? TURN ? x[e] * s[e] + x[4 + e] * c[e] : x[4 + e] : 0.0f;
+        for (int k = 0; k < kTogether; ++k)
+            if (h + k < h1) piece[k].load(src + (h + k) * a.qs[1], sub);
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k) {
+            if (h + k >= h1) break;
+            float x[8], y[8];
+            piece[k].get(x);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                y[e] = live ? TURN ? x[e] * c[e] - x[4 + e] * s[e] : x[e] : 0.0f;
+                y[4 + e] = live ? TURN ? x[e] * s[e] + x[4 + e] * c[e] : x[4 + e] : 0.0f;
+            }
+            store_pairs<T, D, HALF>(dst + (h + k) * a.qos[1], sub, y);
         }
-        store_pairs<T, D, HALF>(dst + h * a.qos[1], sub, y);
     }
 }
 
+// How a launch is cut: CTAs for pages, then CTAs for queries.
+struct Plan {
+    int page_ctas, numbers, kv_per, kv_groups, q_per, q_groups;
+};
+
 template <typename T, int D, bool HALF, bool TURN>
-__global__ void __launch_bounds__(32 * kWarps) paged_append_kernel(const PagedArgs a, int page_ctas)
+__global__ void __launch_bounds__(32 * kWarps) paged_append_kernel(const PagedArgs a, const Plan plan)
 {
-    __shared__ float top[2][kWarps];
+    __shared__ float tops[2][kWarps];
     pdl_wait();
-    if ((int)blockIdx.x < page_ctas) write_page<T, D, HALF, TURN>(a, blockIdx.x, top);
-    else turn_queries<T, D, HALF, TURN>(a, blockIdx.x - page_ctas);
+    if ((int)blockIdx.x < plan.page_ctas) write_page<T, D, HALF, TURN>(a, blockIdx.x, plan.numbers, plan.kv_per, plan.kv_groups, tops);
+    else turn_queries<T, D, HALF, TURN>(a, blockIdx.x - plan.page_ctas, plan.q_per, plan.q_groups);
+}
+
+// Of n heads as many for a warp as leave 32 warps per SM when all tokens' take `warps` a head group.
+int heads_per(int n, long long warps, int sms)
+{
+    const long long groups = (32LL * sms + warps - 1) / warps;
+    return groups >= n ? 1 : (int)((n + groups - 1) / groups);
 }
 
 template <typename T, int D> cudaError_t launch_t(const PagedArgs& a, cudaStream_t st)
 {
-    const int per_cta = kWarps / (a.page / kStep);
-    // pages that a sequence of n new tokens touches: at most n / page + 2, and none is numbered twice
-    const long long pages = a.offsets ? (long long)a.N / a.page + 2LL * a.B : a.B;
-    const long long page_ctas = (pages * a.Hk + per_cta - 1) / per_cta;
+    const int team = a.page / kStep, per_cta = kWarps / team;
     constexpr int rows = kWarps * 32 / (D / 8);
-    const long long ctas = page_ctas + (a.q ? ((long long)a.N + rows - 1) / rows : 0);
+    Plan plan{};
+    // pages that a sequence of n new tokens touches: at most n / page + 2, and none is numbered twice
+    plan.numbers = a.offsets ? a.N / a.page + 2 * a.B : a.B;
+    plan.kv_per = heads_per(a.Hk, 2LL * plan.numbers * team, a.sms);
+    plan.kv_groups = (a.Hk + plan.kv_per - 1) / plan.kv_per;
+    plan.q_per = heads_per(a.Hq, (a.N + rows / kWarps - 1) / (rows / kWarps), a.sms);
+    plan.q_per = (plan.q_per + kTogether - 1) / kTogether * kTogether;
+    plan.q_groups = (a.Hq + plan.q_per - 1) / plan.q_per;
+    plan.page_ctas = (int)((2LL * plan.numbers * plan.kv_groups + per_cta - 1) / per_cta);
+    const long long ctas = plan.page_ctas + (a.q ? ((long long)a.N + rows - 1) / rows * plan.q_groups : 0);
     auto kernel = a.table ? (a.half ? paged_append_kernel<T, D, true, true> : paged_append_kernel<T, D, false, true>)
                           : paged_append_kernel<T, D, false, false>;
-    return launch_dependent(kernel, dim3((unsigned)ctas), dim3(32 * kWarps), 0, st, a, (int)page_ctas);
+    return launch_dependent(kernel, dim3((unsigned)ctas), dim3(32 * kWarps), 0, st, a, plan);
 }
 
 }  // namespace

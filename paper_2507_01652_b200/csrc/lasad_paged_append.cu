@@ -151,19 +151,86 @@ template <int D> __device__ __forceinline__ void angles(const PagedArgs& a, long
     c[0] = u.x, s[0] = u.y, c[1] = u.z, s[1] = u.w, c[2] = v.x, s[2] = v.y, c[3] = v.z, s[3] = v.w;
 }
 
-// The new tokens of sequence b: their place in memory, their number and the first one's position.  A sequence
-// that begins before 0 takes no part.
-struct Fresh {
-    int at, n;
-    long long pos;
-};
-__device__ __forceinline__ Fresh fresh_of(const PagedArgs& a, int b)
+// Rows of e4m3 numbers in 8 channels of a lane, times f (a power of two at most 1) and rounded again: slots slot, slot + by .. of
+// those below n, a few of them in flight.
+template <int kFlight>
+__device__ __forceinline__ void round_again(unsigned char* dst, long long slots, int slot, int by, int n, float f)
 {
-    Fresh f;
-    f.at = a.offsets ? max(0, min(a.offsets[b], a.N)) : b;
-    f.n = a.offsets ? max(0, min(a.offsets[b + 1], a.N) - f.at) : 1;
-    f.pos = a.pos[b];
-    return f;
+    for (; slot < n; slot += by * kFlight) {
+        uint2 old[kFlight];
+#pragma unroll
+        for (int k = 0; k < kFlight; ++k)
+            if (slot + k * by < n) old[k] = *reinterpret_cast<const uint2*>(dst + (slot + k * by) * slots);
+#pragma unroll
+        for (int k = 0; k < kFlight; ++k) {
+            if (slot + k * by >= n) break;
+            uint32_t r[2] = {old[k].x, old[k].y};
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float2 u = from_e4m3(r[e] & 0xffffu), v = from_e4m3(r[e] >> 16);
+                r[e] = to_e4m3(u.x * f, u.y * f) | to_e4m3(v.x * f, v.y * f) << 16;
+            }
+            *reinterpret_cast<uint2*>(dst + (slot + k * by) * slots) = make_uint2(r[0], r[1]);
+        }
+    }
+}
+__device__ __forceinline__ void turn_key(float (&x)[8], const float (&c)[4], const float (&s)[4])
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const double x0 = x[e], x1 = x[4 + e], cd = c[e], sd = s[e];
+        x[e] = (float)(x0 * cd - x1 * sd);
+        x[4 + e] = (float)(x0 * sd + x1 * cd);
+    }
+}
+
+// One new token per sequence: a row of lanes has the key or value of one head, so a warp has D / 8 of them side by side,
+// and what it reads of them is asked for before it is known where they go.
+template <typename T, int D, bool HALF, bool TURN>
+__device__ __forceinline__ void write_token(const PagedArgs& a, int cta)
+{
+    constexpr int LANES = D / 8, ROWS = 32 / LANES;
+    const int lane = threadIdx.x & 31, sub = lane % LANES;
+    const long long all = (long long)a.B * a.Hk, at = (long long)cta * kWarps * ROWS + threadIdx.x / LANES;
+    const bool there = at < 2 * all;                                        // (all lanes stay for the shuffles)
+    const int kv = at >= all, unit = there ? (int)(at - kv * all) : 0, b = unit / a.Hk, h = unit - b * a.Hk;
+    Piece<T, D, HALF> piece;
+    piece.load(static_cast<const T*>(kv && there ? a.v : a.k) + b * (kv && there ? a.vs[0] : a.ks[0]) + h * (kv && there ? a.vs[1] : a.ks[1]), sub);
+    const int pos = a.pos[b], page = pos / a.page, slot = pos - page * a.page;
+    bool live = there && pos >= 0 && page < a.table_pages;
+    const int id = live ? a.block_table[(long long)b * a.table_pages + page] : -1;
+    live = live && id >= 0 && id < a.pages;
+    float* const scale = (kv ? a.vscale : a.kscale) + (long long)id * a.Hk + h;
+    const float was = live && slot > 0 ? *scale : 0.0f;
+    float x[8], size = 0.0f;
+    piece.get(x);
+    if (TURN && !kv && live) {
+        float c[4], s[4];
+        angles<D>(a, pos, sub, c, s);
+        turn_key(x, c, s);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) size = fmaxf(size, finite_size(x[e]));
+#pragma unroll
+    for (int k = LANES / 2; k >= 1; k >>= 1) size = fmaxf(size, __shfl_xor_sync(0xffffffffu, size, k));
+    const float now = fmaxf(power_of_two(scale_exponent(size)), was);       // (the shuffles say that all lanes have read it)
+    unsigned char* const dst = kv ? a.vp + id * a.vps[0] + h * a.vps[1] : a.kp + id * a.kps[0] + h * a.kps[1];
+    const long long slots = kv ? a.vps[2] : a.kps[2];
+    if (live) {
+        if (sub == 0) *scale = now;
+        store_bytes<D, HALF>(dst + slot * slots, sub, x, 1.0f / now);
+    }
+    // where a scale has grown the whole warp rounds the earlier tokens again
+    unsigned grown = __ballot_sync(0xffffffffu, live && slot > 0 && now > was && sub == 0);
+    while (grown) {
+        const int from = __ffs(grown) - 1;
+        grown &= grown - 1;
+        const unsigned long long page_at = __shfl_sync(0xffffffffu, (unsigned long long)dst, from);
+        const long long by = __shfl_sync(0xffffffffu, slots, from);
+        const int n = __shfl_sync(0xffffffffu, slot, from);
+        const float f = __shfl_sync(0xffffffffu, was / now, from);
+        round_again<4>(reinterpret_cast<unsigned char*>(page_at) + sub * 8, by, lane / LANES, ROWS, n, f);
+    }
 }
 
 // A page's keys or values of some heads: `page` / kStep warps (a team), kStep tokens each; head after head, the next one's
@@ -181,27 +248,25 @@ __device__ __forceinline__ void write_page(const PagedArgs& a, int cta, int numb
     const int at = unit / groups, h0 = (unit - at * groups) * per, h1 = min(h0 + per, a.Hk);
     if (at >= numbers) return;
     // the page: of sequence b its page number j (see region_tiles for numbers without a table)
-    int b = at, j = 0;
-    if (a.offsets) {
-        int lo = 0, hi = a.B;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (max(0, min(a.offsets[mid], a.N)) / a.page + 2 * mid <= at) lo = mid;
-            else hi = mid;
-        }
-        b = lo;
-        j = at - (max(0, min(a.offsets[b], a.N)) / a.page + 2 * b);
-        if (j < 0) return;
+    int lo = 0, hi = a.B;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (max(0, min(a.offsets[mid], a.N)) / a.page + 2 * mid <= at) lo = mid;
+        else hi = mid;
     }
-    const Fresh f = fresh_of(a, b);
-    if (f.pos < 0 || f.n <= 0) return;
-    const long long page0 = (f.pos / a.page + j) * a.page;                  // the position of the page's first slot
-    if (page0 >= f.pos + f.n || page0 / a.page >= a.table_pages) return;
+    const int b = lo, j = at - (max(0, min(a.offsets[b], a.N)) / a.page + 2 * b);
+    if (j < 0) return;
+    // its new tokens: their place in memory, their number and the first one's position
+    const int from = max(0, min(a.offsets[b], a.N)), n = max(0, min(a.offsets[b + 1], a.N) - from);
+    const long long pos = a.pos[b];
+    if (pos < 0 || n == 0) return;
+    const long long page0 = (pos / a.page + j) * a.page;                    // the position of the page's first slot
+    if (page0 >= pos + n || page0 / a.page >= a.table_pages) return;
     const int id = a.block_table[(long long)b * a.table_pages + page0 / a.page];
     if (id < 0 || id >= a.pages) return;
     // slots first .. last - 1 are new; the row of slot 0
-    const int first = (int)max(0LL, f.pos - page0), last = (int)min((long long)a.page, f.pos + f.n - page0);
-    const long long row0 = f.at + (page0 - f.pos), stride = kv ? a.vs[0] : a.ks[0], next_head = kv ? a.vs[1] : a.ks[1];
+    const int first = (int)max(0LL, pos - page0), last = (int)min((long long)a.page, pos + n - page0);
+    const long long row0 = from + (page0 - pos), stride = kv ? a.vs[0] : a.ks[0], next_head = kv ? a.vs[1] : a.ks[1];
     const T* src = static_cast<const T*>(kv ? a.v : a.k) + (row0 + w * kStep + mine) * stride;
     const long long slots = kv ? a.vps[2] : a.kps[2];
     auto fresh = [&](int i) {
@@ -231,14 +296,7 @@ __device__ __forceinline__ void write_page(const PagedArgs& a, int cta, int numb
         for (int i = 0; i < ACC; ++i) {
             if (!fresh(i)) continue;
             now[i].get(x[i]);
-            if (TURN && kv == 0) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const double x0 = x[i][e], x1 = x[i][4 + e], cd = c[i][e], sd = s[i][e];
-                    x[i][e] = (float)(x0 * cd - x1 * sd);
-                    x[i][4 + e] = (float)(x0 * sd + x1 * cd);
-                }
-            }
+            if (TURN && kv == 0) turn_key(x[i], c[i], s[i]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) size = fmaxf(size, finite_size(x[i][e]));
         }
@@ -255,20 +313,7 @@ __device__ __forceinline__ void write_page(const PagedArgs& a, int cta, int numb
         }
         const float now_s = fmaxf(power_of_two(scale_exponent(size)), was);
         if (w == 0 && lane == 0) *scale = now_s;
-        if (first > 0 && now_s > was) {
-            const float f8 = was / now_s;
-            for (int slot = w * ROWS + mine; slot < first; slot += W * ROWS) {
-                unsigned char* row = dst + slot * slots + sub * 8;
-                uint2 old = *reinterpret_cast<const uint2*>(row);
-                uint32_t r[2] = {old.x, old.y};
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float2 u = from_e4m3(r[e] & 0xffffu), v = from_e4m3(r[e] >> 16);
-                    r[e] = to_e4m3(u.x * f8, u.y * f8) | to_e4m3(v.x * f8, v.y * f8) << 16;
-                }
-                *reinterpret_cast<uint2*>(row) = make_uint2(r[0], r[1]);
-            }
-        }
+        if (first > 0 && now_s > was) round_again<1>(dst + sub * 8, slots, w * ROWS + mine, W * ROWS, first, was / now_s);
         const float inv = 1.0f / now_s;
 #pragma unroll
         for (int i = 0; i < ACC; ++i) {
@@ -279,7 +324,7 @@ __device__ __forceinline__ void write_page(const PagedArgs& a, int cta, int numb
 }
 
 // A row of lanes has a token and some of its query heads, kTogether at a time.
-constexpr int kTogether = 4;
+constexpr int kTogether = 8;
 template <typename T, int D, bool HALF, bool TURN>
 __device__ __forceinline__ void turn_queries(const PagedArgs& a, int cta, int per, int groups)
 {
@@ -337,13 +382,16 @@ struct Plan {
     int page_ctas, numbers, kv_per, kv_groups, q_per, q_groups;
 };
 
-template <typename T, int D, bool HALF, bool TURN>
-__global__ void __launch_bounds__(32 * kWarps) paged_append_kernel(const PagedArgs a, const Plan plan)
+// STEP: one token per sequence.  (Two CTAs have an SM: with one, prompts of 8 x 9217 tokens take 250 us instead of 140.)
+template <typename T, int D, bool HALF, bool TURN, bool STEP>
+__global__ void __launch_bounds__(32 * kWarps, 2) paged_append_kernel(const PagedArgs a, const Plan plan)
 {
     __shared__ float tops[2][kWarps];
     pdl_wait();
-    if ((int)blockIdx.x < plan.page_ctas) write_page<T, D, HALF, TURN>(a, blockIdx.x, plan.numbers, plan.kv_per, plan.kv_groups, tops);
-    else turn_queries<T, D, HALF, TURN>(a, blockIdx.x - plan.page_ctas, plan.q_per, plan.q_groups);
+    if ((int)blockIdx.x < plan.page_ctas) {
+        if constexpr (STEP) write_token<T, D, HALF, TURN>(a, blockIdx.x);
+        else write_page<T, D, HALF, TURN>(a, blockIdx.x, plan.numbers, plan.kv_per, plan.kv_groups, tops);
+    } else turn_queries<T, D, HALF, TURN>(a, blockIdx.x - plan.page_ctas, plan.q_per, plan.q_groups);
 }
 
 // Of n heads as many for a warp as leave 32 warps per SM when all tokens' take `warps` a head group.
@@ -359,16 +407,18 @@ template <typename T, int D> cudaError_t launch_t(const PagedArgs& a, cudaStream
     constexpr int rows = kWarps * 32 / (D / 8);
     Plan plan{};
     // pages that a sequence of n new tokens touches: at most n / page + 2, and none is numbered twice
-    plan.numbers = a.offsets ? a.N / a.page + 2 * a.B : a.B;
+    plan.numbers = a.N / a.page + 2 * a.B;
     plan.kv_per = heads_per(a.Hk, 2LL * plan.numbers * team, a.sms);
     plan.kv_groups = (a.Hk + plan.kv_per - 1) / plan.kv_per;
     plan.q_per = heads_per(a.Hq, (a.N + rows / kWarps - 1) / (rows / kWarps), a.sms);
     plan.q_per = (plan.q_per + kTogether - 1) / kTogether * kTogether;
     plan.q_groups = (a.Hq + plan.q_per - 1) / plan.q_per;
-    plan.page_ctas = (int)((2LL * plan.numbers * plan.kv_groups + per_cta - 1) / per_cta);
+    plan.page_ctas = a.offsets ? (int)((2LL * plan.numbers * plan.kv_groups + per_cta - 1) / per_cta) : (int)((2LL * a.B * a.Hk + rows - 1) / rows);
     const long long ctas = plan.page_ctas + (a.q ? ((long long)a.N + rows - 1) / rows * plan.q_groups : 0);
-    auto kernel = a.table ? (a.half ? paged_append_kernel<T, D, true, true> : paged_append_kernel<T, D, false, true>)
-                          : paged_append_kernel<T, D, false, false>;
+    auto kernel = a.offsets ? (a.table ? (a.half ? paged_append_kernel<T, D, true, true, false> : paged_append_kernel<T, D, false, true, false>)
+                                       : paged_append_kernel<T, D, false, false, false>)
+                            : (a.table ? (a.half ? paged_append_kernel<T, D, true, true, true> : paged_append_kernel<T, D, false, true, true>)
+                                       : paged_append_kernel<T, D, false, false, true>);
     return launch_dependent(kernel, dim3((unsigned)ctas), dim3(32 * kWarps), 0, st, a, plan);
 }
 

@@ -197,6 +197,89 @@ def test_packed_offsets_that_do_not_ascend_stay_inside(ctx):      # noqa: F811
     assert ctx.device_status() == 0
 
 
+def both_ways(ctx, dev, at, **kw):      # noqa: F811
+    """What the tensor cores and the CUDA cores make of it."""
+    q, k, v, do = dev
+    out = []
+    try:
+        for impl in (2, 1):
+            ctx.set_option(binding.LASAD_OPT_WINDOW_IMPL, impl)
+            o, lse = ctx.lasad_packed_attention(q, k, v, at, want_lse=True, **kw)
+            out.append((o, lse) + ctx.lasad_packed_attention_backward(q, k, v, o, lse, do, at, **kw))
+    finally:
+        ctx.set_option(binding.LASAD_OPT_WINDOW_IMPL, 0)
+    return out
+
+
+@pytest.mark.parametrize("lengths,tail,Hq,Hk,d", [
+    ((257,) * 32, 0, 12, 12, 64), ((129,) * 40, 5, 16, 4, 64), ((1,) * 300, 0, 8, 8, 64), ((3000, 1, 300, 2049), 700, 6, 2, 64),
+    ((1025,) * 4, 0, 24, 8, 64), ((0, 640, 0, 0, 641, 1) * 6, 3, 10, 5, 32), ((65, 64, 63) * 50, 0, 5, 1, 64)])
+def test_packed_many_units_on_both_implementations(ctx, lengths, tail, Hq, Hk, d):      # noqa: F811
+    """So many units that every CTA takes several, some of which one of its row tiles has none of: both
+    implementations round p and ds and their outputs by at most 2^-8 each, so they are within 2^-7 of one another in the
+    2-norm (the statistics, in fp32, within 2^-18).  Where rows see one key dP - Delta is 0, and what is left of it is the fp32
+    rounding of sums of 64 products of size 1, |do||v| 2^-23 or less, on keys of size 1: 2^-18 for an element is far above."""
+    _, dev, offsets, at = packed_case(lengths, tail, Hq, Hk, d, BF16, 3)
+    for name, a, b in zip(("o", "lse", "dq", "dk", "dv"), *both_ways(ctx, dev, at)):
+        a, b = a.double(), b.double()
+        if name == "lse":
+            live = b > -math.inf
+            assert torch.equal(live, a > -math.inf) and float((a - b)[live].abs().max()) <= 2.0 ** -18 * float(b[live].abs().max())
+        else:
+            assert float((a - b).norm()) <= 2.0 ** -7 * float(b.norm()) + 2.0 ** -18 * math.sqrt(b.numel()), name
+            assert bool((a[offsets[-1]:] == 0).all())
+    assert ctx.device_status() == 0
+
+
+def test_packed_back_to_back_in_a_warm_cache(ctx):      # noqa: F811
+    """Over and over with nothing in between: no wait may give up, and every launch returns the same bits."""
+    _, (q, k, v, do), _, at = packed_case((2305, 700, 129, 1), 0, 8, 4, 64, BF16, 6)
+    first = None
+    for _ in range(30):
+        o, lse = ctx.lasad_packed_attention(q, k, v, at, want_lse=True)
+        got = (o, lse) + ctx.lasad_packed_attention_backward(q, k, v, o, lse, do, at)
+        first = first or got
+    torch.cuda.synchronize()
+    assert ctx.device_status() == 0
+    assert all(torch.equal(a, b) for a, b in zip(first, got))
+
+
+def test_packed_waits_are_bounded(ctx):      # noqa: F811
+    """Waits that run out after one try: the kernels report it and leave, and the next calls are whole."""
+    _, (q, k, v, do), _, at = packed_case((700, 300), 0, 4, 4, 64, BF16, 7)
+    o, lse = ctx.lasad_packed_attention(q, k, v, at, want_lse=True)
+    want = ctx.lasad_packed_attention_backward(q, k, v, o, lse, do, at)
+    try:
+        ctx.set_option(binding.LASAD_OPT_WAIT_LIMIT, 1)
+        ctx.lasad_packed_attention(q, k, v, at)
+        torch.cuda.synchronize()
+        assert ctx.device_status() == binding.LASAD_ERR_TIMEOUT
+        ctx.lasad_packed_attention_backward(q, k, v, o, lse, do, at)
+        torch.cuda.synchronize()
+        assert ctx.device_status() == binding.LASAD_ERR_TIMEOUT
+    finally:
+        ctx.set_option(binding.LASAD_OPT_WAIT_LIMIT, 0)
+    assert torch.equal(ctx.lasad_packed_attention(q, k, v, at)[0], o)
+    assert all(torch.equal(a, b) for a, b in zip(ctx.lasad_packed_attention_backward(q, k, v, o, lse, do, at), want))
+    assert ctx.device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_packed_rows_far_apart(ctx, dtype):      # noqa: F811
+    """Places past 2^31 elements: rows 8 M elements apart."""
+    host, dev, offsets, at = packed_case((150, 130), 0, 2, 1, 64, dtype, 9)
+    o, lse = ctx.lasad_packed_attention(*dev[:3], at, want_lse=True)
+    want = (o,) + ctx.lasad_packed_attention_backward(*dev[:3], o, lse, dev[3], at)
+    apart = 8 << 20
+    big = torch.zeros(280 * apart, dtype=dtype, device="cuda")
+    view = lambda n, t: torch.as_strided(big, t.shape, (apart, 64, 1), n * 256)       # noqa: E731
+    far = [view(n, t).copy_(t) for n, t in enumerate((*dev, o))]
+    outs = [view(8 + n, t) for n, t in enumerate(want)]
+    ctx.lasad_packed_attention(*far[:3], at, o=outs[0], lse=lse)
+    ctx.lasad_packed_attention_backward(*far[:3], far[4], lse, far[3], at, dq=outs[1], dk=outs[2], dv=outs[3])
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
 # ---------------------------------------------------------------------------------------------
 # paged cache
 # ---------------------------------------------------------------------------------------------
@@ -389,6 +472,63 @@ def test_paged_attention_a_nan_stays_in_its_sequence(ctx):      # noqa: F811
     b, _ = ctx.lasad_paged_attention(q, **to_dev(cache), block_table=bt, pos=pos)
     assert torch.equal(a[1], b[1]) and torch.equal(a[0, 2:], b[0, 2:])
     assert bool(b[0, :2, 7].isnan().all()) and bool(b[0, :2, :7].isfinite().all())
+
+
+def test_pages_far_apart_and_tokens_first(ctx):      # noqa: F811
+    """A pool whose pages are 3 GiB apart (places past 2^32 bytes), and one with the slots ahead of the heads."""
+    g = gen(12)
+    cache = cache_of(g, 4, 2, 16, 64, low=-9, high=-6)
+    bt, pos = torch.tensor([[3, 0, 2, 1]], dtype=torch.int32).cuda(), torch.tensor([49], dtype=torch.int32, device="cuda")
+    k, v, q = (rnd(g, 1, h, 64, dtype=BF16).cuda() for h in (2, 2, 4))
+    apart = 3 << 30
+    big = torch.zeros(3 * apart + (1 << 20), dtype=torch.uint8, device="cuda").view(E4M3)
+    results = []
+    for how in ("together", "apart", "tokens first"):
+        dev = to_dev(cache)
+        for n, name in enumerate(("k_pages", "v_pages")):
+            t = dev[name]
+            if how == "apart":
+                dev[name] = torch.as_strided(big, t.shape, (apart, 16 * 64, 64, 1), n * 4096)
+            elif how == "tokens first":
+                dev[name] = torch.empty(4, 16, 2, 64, dtype=torch.uint8, device="cuda").view(E4M3).transpose(1, 2)
+            if how != "together":
+                dev[name].view(torch.uint8).copy_(t.view(torch.uint8))
+        ctx.lasad_paged_append(k, v, **dev, block_table=bt, pos=pos)
+        o, lse = ctx.lasad_paged_attention(q, **dev, block_table=bt, pos=pos, want_lse=True)
+        results.append([o, lse] + [dev[n].view(torch.uint8).clone() for n in ("k_pages", "v_pages")] + [dev["k_scales"], dev["v_scales"]])
+    for other in results[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(results[0], other))
+
+
+@pytest.mark.parametrize("shape", [(300, 4, 4, 40), (40, 24, 8, 700), (2, 6, 2, 3000), (1, 24, 1, 5000)])
+def test_paged_attention_by_every_plan(ctx, shape):      # noqa: F811
+    """A warp, a CTA and many CTAs for a (sequence, key head): against the attention of a prompt's last token over the cache's
+    own values, in float64 on the device."""
+    B, Hq, Hk, n = shape
+    g, page = gen(B), 32
+    entries = -(-n // page)
+    cache = to_dev(cache_of(g, B * entries, Hk, page, 64, low=-9, high=-6))
+    bt = torch.randperm(B * entries, generator=g).view(B, entries).int().cuda()
+    pos = torch.randint(-1, n, (B,), generator=g).int()
+    pos[-1] = n - 1
+    for dtype in (F32, BF16):
+        q = rnd(g, B, Hq, 64, dtype=dtype).cuda()
+        got, lse = ctx.lasad_paged_attention(q, **cache, block_table=bt, pos=pos.cuda(), want_lse=True)
+        for b in list(range(min(B, 12))) + [B - 1]:
+            if int(pos[b]) < 0:
+                assert bool((got[b] == 0).all()) and bool((lse[b] == -math.inf).all())
+                continue
+            kk, vv = ((cache[m + "_pages"][bt[b].long()].double() * cache[m + "_scales"][bt[b].long()].double()[..., None, None])
+                      .transpose(0, 1).flatten(1, 2)[:, : int(pos[b]) + 1].repeat_interleave(Hq // Hk, 0) for m in ("k", "v"))
+            x = torch.einsum("hd,hnd->hn", q[b].double(), kk) / 8
+            p = torch.softmax(x, -1)
+            o = torch.einsum("hn,hnd->hd", p, vv)
+            # weights: 2^-11 (bf16) or 2^-22; exponents 2^-20 of their size; the output's own rounding
+            size = torch.einsum("hd,hnd->hn", q[b].double().abs(), kk.abs()) / 8
+            e = (2.0 ** -11 if dtype == BF16 else 2.0 ** -22) + 2.0 ** -20 * (2 + size + x.abs().amax(-1, keepdim=True))
+            bound = torch.einsum("hn,hnd->hd", p * e, vv.abs()) + torch.finfo(dtype).eps / 2 * o.abs() + 2.0 ** -30
+            assert bool(((got[b].double() - o).abs() <= 1.02 * bound).all()), (b, dtype)
+            near(lse[b], torch.logsumexp(x, -1).cpu(), F32, "lse", extra=2.0 ** -18)
 
 
 # ---------------------------------------------------------------------------------------------

@@ -18,12 +18,14 @@
 // 2^8, far inside the range of fp32 and bf16; after the first tiles rare) m moves, O and l are scaled and P is formed
 // again.
 //
-// Measured: 1 x 9217 tokens, 24 query and 8 key heads: 417 us, 626 TFLOP/s of the pairs that count, exponentials 54 % busy;
-// 64 sequences of 1 to 577 tokens, 16 and 4 heads: 60 us.  A group alone takes 1130 clocks for a tile, 600 of them
-// exponentials, the two together 1560 for two: they meet in the exponentials again and again, also when one is made to
-// start late.  Tried and no faster: tiles of 128 keys (421), sixteen warps on even and odd tiles (417), three
-// groups (450), a quarter of the exponentials as polynomials (419), S issued right behind the product (429), masked and other
-// tiles as two bodies (443), a short rolled body (462).
+// Measured: 1 x 9217 tokens, 24 query and 8 key heads: 418 us, 624 TFLOP/s of the pairs that count, the pipe of the
+// exponentials issuing on 56 % of the clocks; 64 sequences of 1 to 577 tokens, 16 and 4 heads: 61 us.  With clocks read
+// in the loop (which slows it a little) a group alone takes 1290 clocks for a tile, 740 of them from the scores to P, the two
+// groups together 1775 to 1800 for two tiles: they meet in the exponentials, also when one is made to start late (424 to
+// 450 us).  Tried on that case: 128-key tiles 421, with a quarter of the exponentials as polynomials 412 (tiles of 64 with an
+// eighth, a quarter, three eighths: 429, 419, 444); sixteen warps on even and odd tiles 417; three groups 450 (and 83
+// instead of 61 us on the short sequences); S issued right behind the product 429; masked and other tiles as two
+// bodies 443; a short rolled body 462.
 //
 // P is rounded to bf16 where it enters P V, as the tensor cores take it beside bf16 values: 2^-9 of each term, which
 // adds up like noise (l sums the P that were not rounded).

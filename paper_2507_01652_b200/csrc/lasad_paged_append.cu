@@ -18,9 +18,9 @@
 //
 // Bound by memory: k, v and q in, a byte a value and q out.  Prompts: a page's keys, or values, of some heads for a team of
 // page / 16 warps, so that its maximum needs no second reading, the next head's rows on their way meanwhile; queries by CTAs of
-// their own, eight heads at a time (8 x 9217 tokens, 24 query and 8 key heads, 680 MB: 139 us, 4.9 TB/s; keys, then values, by
-// the same warps and one query head at a time 326).  One token per sequence: 3.8 us for 256 x 20 heads (by the prompts'
-// kernel, where 15 of 16 rows of lanes have nothing to do, 11.6).
+// their own, eight heads at a time (8 x 9217 tokens, 24 query and 8 key heads, 680 MB: 139 us, 4.9 TB/s; four heads at a time 154;
+// keys, then values, by the same warps and one query head at a time 326).  One token per sequence: 3.8 us for 256 x 20 heads (by the prompts'
+// kernel 11.6).
 #include "lasad_full.cuh"
 #include "lasad_tc_ptx.cuh"
 

@@ -5,13 +5,13 @@
 // Bound by reading the cache once, 2 d bytes a token and key head.  A warp takes steps of 16 tokens, copied to shared
 // memory three (d = 64) or seven steps ahead, and from there into the fragments of two products on mma.sync.m16n8k16:
 // tokens are the rows of the first, channels those of the second; the columns are the query heads that share the key
-// head, 8 at a time, of which few are used, so the tensor cores have time to spare (12 % busy) and tcgen05's 128 rows
+// head, 8 at a time, of which few are used, so the tensor cores have time to spare and tcgen05's 128 rows
 // would only be emptier.  e4m3 numbers are exact in fp16, so keys and values enter without a rounding; the page's key
 // scale multiplies the fp32 score.  The order of a product's inner index is free, and so is that of its rows, so a lane
 // reads 16 neighbouring channels of a key and 8 of a value.
 // Measured: 64 sequences of 9217 tokens, 24 query and 8 key heads: 5.9 TB/s (loads into registers three steps ahead, which
-// were waited for all the same, 4.65; steps of 16 KB a warp instead of 8, so two CTAs fewer on an SM, 5.3); of 1 to 9217
-// tokens 64 us, 4.7 TB/s: CTAs of short parts spend their time on the chain position - page - rows.
+// were waited for all the same, 4.65; twice as many steps on their way 5.3); of 1 to 9217
+// tokens 64.8 us, 4.7 TB/s.
 //
 // The page's value scale goes into the exponent: with x_j = scale q.k_j log2(e) + log2 s_j a warp sums
 //
@@ -24,9 +24,10 @@
 // so that fp16 holds it.
 //
 // The tokens of a sequence are cut into parts where there are few (sequence, key head) pairs; then the parts'
-// (M, l, O) go to memory and a second kernel joins them (2 x 24 heads of 8 key heads, 9217 tokens: 9.5 us; the CTAs of a
-// cluster that join in shared memory 12.7).  Where there are many a warp has one (256 x 20 heads, up to 577 tokens: 40
-// us; four warps 50).
+// (M, l, O) go to memory and a second kernel joins them (2 x 24 heads of 8 key heads, 9217 tokens: 9.5 us; joined by the
+// CTAs of a cluster in shared memory 12.7, where two kernels then took 11.6).  Twice or half as many parts: 69.4 or 66.7 us
+// for 64 sequences of 1 to 9217 tokens, as it is 64.8.  Where there are many pairs a warp has one (256 x 20 heads, up to
+// 577 tokens: 40.6 us; four warps 49.6).
 #include "lasad_full.cuh"
 #include "lasad_tc_ptx.cuh"
 #include "lasad_tc_tma.cuh"

@@ -125,7 +125,8 @@ class Sequences:
     def _paged(self, key, q, k, v, o, k_pages, v_pages, k_scales, v_scales, block_table, pos, offsets, table, grid, lse):
         """Checks a call that looks like none before it."""
         self._here(q, k, v, o, k_pages, v_pages, k_scales, v_scales, block_table, pos, offsets, table, lse)
-        for n, t in (("k_pages", k_pages), ("v_pages", v_pages), ("block_table", block_table), ("pos", pos), ("k_scales", k_scales), ("v_scales", v_scales)):
+        for n, t in (("k_pages", k_pages), ("v_pages", v_pages), ("block_table", block_table), ("pos", pos),
+                     ("k_scales", k_scales), ("v_scales", v_scales)):
             if t is None:
                 raise ValueError(f"{n} is missing")
         first = k if q is None else q

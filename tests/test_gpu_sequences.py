@@ -557,7 +557,6 @@ def test_prompts_then_tokens(ctx, dtype):      # noqa: F811
     ref.append(k, v, want, bt, [0] * B, offsets, table, w, prefix)
     same_cache(dev, want)
     # packed attention on the same rotation
-    _, kt = ctx.lasad_qk_norm_rope(q[None].cuda(), k[None].cuda(), table.cuda(), grid_w=w, prefix_len=prefix)   # (norm: not used)
     kt = torch.cat([torch.stack([ref.turned(d64(k[offsets[b] + i]), table, i, w, prefix) for i in range(n)])
                     for b, n in enumerate(prompts) if n]).to(dtype)
     o, _ = ctx.lasad_packed_attention(qt, kt.cuda(), v.cuda(), at)

@@ -107,15 +107,22 @@ def test_other_shapes_and_types_are_refused(world, call, name):      # noqa: F81
     else:
         more = lambda i: [n + (1 if i == j else 0) for j, n in enumerate(t.shape)]   # noqa: E731
         bad = [m(*more(i), dtype=t.dtype) for i in range(t.dim())] + [m(*t.shape, dtype=torch.float64), m(*t.shape, 1, dtype=t.dtype)]
+    free = {"table": 0, "block_table": 1}      # another number of rows of the table, or of pages of a sequence, is a call
+    if call != "lasad_paged_append":
+        free["offsets"] = 0                    # and so is another number of sequences where nothing else counts them
+    if name in free:
+        del bad[free[name]]
     for other in bad:
-        if name in ("offsets", "block_table", "table") and call != "lasad_paged_append" or (call, name) == ("lasad_paged_append", "table"):
-            if other.dtype == t.dtype and other.dim() == t.dim() and name != "lse" and (name, tuple(other.shape)) not in (
-                    ("table", (9, 33, 2)), ("table", (9, 32, 3)), ("block_table", (3, 3))):
-                continue             # another number of sequences, pages of a sequence or rows of the table
-        if name == "block_table" and tuple(other.shape) == (2, 4):
-            continue
         with pytest.raises((ValueError, TypeError)):
             getattr(ctx, call)(**{**kw, name: other})
+
+
+@pytest.mark.parametrize("call", ["lasad_paged_append", "lasad_paged_attention"])
+@pytest.mark.parametrize("name", ["k_pages", "v_pages", "v_scales"])
+def test_a_cache_is_asked_for_whole(world, call, name):      # noqa: F811
+    ctx, _ = world
+    with pytest.raises(ValueError, match=name):
+        getattr(ctx, call)(**{**arguments()[call], name: None})
 
 
 @pytest.mark.parametrize("call,name", [(c, n) for c, n in CASES if n in ("offsets", "block_table", "pos", "k_scales")

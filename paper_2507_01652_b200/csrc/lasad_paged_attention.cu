@@ -468,19 +468,22 @@ __global__ void __launch_bounds__(32 * kJoinWarps) paged_join_kernel(const Paged
         float top = M;
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
-            if (p0 + k * kJoinWarps >= parts) m[k] = -INFINITY, l[k] = 0.0f;
+            if (p0 + k * kJoinWarps >= parts) {              // (memory that nobody has written)
+                m[k] = -INFINITY, l[k] = 0.0f;
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[k][e] = 0.0f;
+            }
             top = fmaxf(top, m[k]);
         }
-        if (top == -INFINITY) continue;
-        const float f0 = tcx::ex2_approx(M - top);
+        // (a part without a maximum is added, too: its sums are 0, or NaN where its scores are, and that has to stay)
+        const float base = top == -INFINITY ? 0.0f : top, f0 = tcx::ex2_approx(M - base);
         M = top;
         L *= f0;
 #pragma unroll
         for (int e = 0; e < E; ++e) O[e] *= f0;
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
-            if (m[k] == -INFINITY) continue;
-            const float f = tcx::ex2_approx(m[k] - M);
+            const float f = tcx::ex2_approx(m[k] - base);
             L = fmaf(l[k], f, L);
 #pragma unroll
             for (int e = 0; e < E; ++e) O[e] = fmaf(o[k][e], f, O[e]);

@@ -474,6 +474,31 @@ def test_paged_attention_a_nan_stays_in_its_sequence(ctx):      # noqa: F811
     assert bool(b[0, :2, 7].isnan().all()) and bool(b[0, :2, :7].isfinite().all())
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("entries", [4, 130])       # one part, and parts that are joined
+def test_paged_attention_keeps_a_nan_of_the_query(ctx, entries, dtype):      # noqa: F811
+    """Where every score of a sequence is NaN so is its output, however its tokens are cut.  Other sequences and key
+    heads keep their bits.  The head that shares the key head shares the warps, which move their running maximum as soon as
+    one column has none, and so at other steps than before: a move multiplies by an exponential (2^-22), a warp has at most
+    4 steps of a part here (256 tokens, 4 warps, 16 tokens a step), and 4 x 2^-22 is below the 2 x 2^-20 that the
+    formula's bound has for exponentials.  So it is held to that bound."""
+    g = gen(10)
+    cache = cache_of(g, entries, 2, 16, 64, low=-9, high=-6)
+    bt = torch.arange(entries).int().repeat(3, 1).cuda()
+    pos = torch.tensor([16 * entries - 1, 16 * entries - 1, -1], dtype=torch.int32, device="cuda")
+    q = rnd(g, 3, 4, 64, dtype=dtype).cuda()
+    a, la = ctx.lasad_paged_attention(q, **to_dev(cache), block_table=bt, pos=pos, want_lse=True)
+    q[1, 2, 5] = float("nan")
+    b, lb = ctx.lasad_paged_attention(q, **to_dev(cache), block_table=bt, pos=pos, want_lse=True)
+    assert bool(b[1, 2].isnan().all()) and bool(lb[1, 2].isnan())
+    o, lse, err = ref.paged(d64(q[:2, 3:]).repeat(1, 2, 1), {n: x[:, 1:] for n, x in to_64(cache).items()}, bt.cpu(),
+                            pos[:2].tolist(), u=2.0 ** -11 if dtype == BF16 else 2.0 ** -22)
+    inside("the other head", b[1, 3], o[1, 0], err[1, 0] + torch.finfo(dtype).eps / 2 * o[1, 0].abs())
+    near(lb[1, 3], lse[1, 0], F32, "lse", extra=2.0 ** -18)
+    b[1, 2:], lb[1, 2:] = a[1, 2:], la[1, 2:]
+    assert torch.equal(a, b) and torch.equal(la, lb)
+
+
 def test_pages_far_apart_and_tokens_first(ctx):      # noqa: F811
     """A pool whose pages are 3 GiB apart (places past 2^32 bytes), and one with the slots ahead of the heads."""
     g = gen(12)

@@ -521,7 +521,8 @@ int lasad_paged_append(lasad_ctx* ctx, const lasad_paged_params* p, const void* 
  * (the token's own among them: append it first).  lse [B,Hq] fp32 or NULL.  A sequence with a negative position, or
  * that sees no page, has o = 0 and lse = -infinity.  Scores, statistics and sums are fp32; with bf16 the weights
  * are rounded to fp16 where they meet the values (2^-11), with f32 nothing is rounded below 22 bits.
- * table_pages * page <= 2^30; pages times the page stride < 64 GiB.
+ * table_pages * page <= 2^30; from a head's first slot of the first page to its last of the last less than 64 GiB.
+ * Scales are what the append leaves, finite and greater than 0.
  */
 int64_t lasad_paged_attention_workspace(lasad_ctx* ctx, const lasad_paged_params* p);
 int lasad_paged_attention(lasad_ctx* ctx, const lasad_paged_params* p, const void* q, const void* k_pages,

@@ -79,6 +79,12 @@ bool pages_ok(const int64_t* s, const lasad_paged_params* p, long long (&to)[3])
     }
     return (s[0] > 0 || p->pages == 1) && (s[1] >= p->d || p->Hk == 1) && s[2] >= p->d;
 }
+// Whether a head's last slot of the last page begins less than 2^32 - 1 times 16 bytes behind its first of the first.
+bool places_fit(const int64_t* s, const lasad_paged_params* p)
+{
+    const int64_t limit = 0xffffffffLL * 16;
+    return s[0] < limit && s[2] < limit && (p->pages - 1) * (s[0] / 16) + (p->page - 1) * (s[2] / 16) < 0xffffffffLL;
+}
 int paged_args(lasad_ctx* ctx, const lasad_paged_params* p, bool append, bool queries, bool packed, bool turn, lasad::PagedArgs& a)
 {
     if (!ctx || !p) return LASAD_ERR_INVALID_ARG;
@@ -99,8 +105,7 @@ int paged_args(lasad_ctx* ctx, const lasad_paged_params* p, bool append, bool qu
         (int64_t)p->table_pages * p->page > (1 << 30))
         return LASAD_ERR_UNSUPPORTED;
     // (places in the pool are counted in 16 bytes and 32 bits)
-    if (!append && (p->pages * (p->k_pages_stride[0] / 16) >= 0xffffffffLL || p->pages * (p->v_pages_stride[0] / 16) >= 0xffffffffLL))
-        return LASAD_ERR_UNSUPPORTED;
+    if (!append && !(places_fit(p->k_pages_stride, p) && places_fit(p->v_pages_stride, p))) return LASAD_ERR_UNSUPPORTED;
     // (the units of a launch are counted in 32 bits)
     if (append ? p->N > (1 << 30) || 2 * ((int64_t)p->N / p->page + 2LL * p->B) * p->Hk + (int64_t)p->N * p->Hq > 0x7fffffffLL
                : (int64_t)p->B * p->Hq * 256 > 0x7fffffffLL)

@@ -3,12 +3,13 @@
 Bounds come from the arithmetic, as in test_gpu_mixers: what a rounding to the type of the weights or of the output
 costs (bf16 2^-8, both sides of it), and 2^-20 of the sum of magnitudes for fp32 sums and exponentials.  What
 is rounded to 8 bits is compared for equality."""
+import ctypes
 import math
 
 import pytest
 import torch
 
-from paper_2507_01652_b200 import binding
+from paper_2507_01652_b200 import binding, sequences
 from tests import _sequences_ref as ref
 from tests.test_gpu_mixers import BF16, F32, ctx, d64, gen, near, rnd, strided  # noqa: F401
 
@@ -497,6 +498,20 @@ def test_paged_attention_keeps_a_nan_of_the_query(ctx, entries, dtype):      # n
     near(lb[1, 3], lse[1, 0], F32, "lse", extra=2.0 ** -18)
     b[1, 2:], lb[1, 2:] = a[1, 2:], la[1, 2:]
     assert torch.equal(a, b) and torch.equal(la, lb)
+
+
+@pytest.mark.parametrize("strides", [(64, 64, 1 << 30), (1 << 31, 64, 64), (64, 64, 1 << 62), (1 << 62, 64, 64)])
+@pytest.mark.parametrize("which", ["k_pages_stride", "v_pages_stride"])
+def test_pools_too_large_to_count_are_refused(ctx, which, strides):      # noqa: F811
+    """The last place of a pool decides, whichever stride takes it there.  (Asking for the workspace launches nothing.)"""
+    p = sequences.PagedParams(2, 0, 4, 2, 64, 1, 128, 64, 4, 0, 0, 0, 0, 0.125)
+    for n in ("k_pages_stride", "v_pages_stride"):
+        setattr(p, n, (ctypes.c_int64 * 3)(2 * 128 * 64, 128 * 64, 64))
+    for n in ("q_stride", "o_stride"):
+        setattr(p, n, (ctypes.c_int64 * 2)(256, 64))
+    assert ctx._lib.lasad_paged_attention_workspace(ctx._h, ctypes.byref(p)) >= 0
+    setattr(p, which, (ctypes.c_int64 * 3)(*strides))
+    assert ctx._lib.lasad_paged_attention_workspace(ctx._h, ctypes.byref(p)) == binding.LASAD_ERR_UNSUPPORTED
 
 
 def test_pages_far_apart_and_tokens_first(ctx):      # noqa: F811

@@ -377,6 +377,8 @@ __device__ __forceinline__ void softmax_rows(const Params& p, Smem& sm, int g, i
                 }
                 top = exponentials(sv, p.scale2, m == -INFINITY ? 0.0f : -m, at_p, l) * p.scale2;
                 if (__any_sync(0xffffffffu, top > m + 8.0f || (m == -INFINITY && top > m))) {
+                    // (P is written again below, to the same columns: stores are in no order until they are waited for)
+                    tmem_wait_st();
                     // (every row of the warp moves to its maximum now, or its turn would come one by one)
                     now = fmaxf(m, top);
                     const float f = now == m ? 1.0f : ex2_approx(m - now);

@@ -1,0 +1,60 @@
+"""Packed attention where the running maximum of a row moves: P of the tile is formed again, and O and the sum are
+scaled.  With scores of ordinary size that is rare after a sequence's first tile, so these make it happen."""
+import math
+
+import pytest
+import torch
+
+from paper_2507_01652_b200 import binding  # noqa: F401
+from tests import _sequences_ref as ref
+from tests.test_gpu_mixers import BF16, F32, ctx, d64, gen, near, rnd  # noqa: F401
+from tests.test_gpu_sequences import inside
+
+pytestmark = pytest.mark.gpu
+
+
+def growing(T, heads, seed, step=14.0):
+    """Keys whose score grows by ``step`` (in log2) or a little more from one tile of 64 to the next, for every query."""
+    g = gen(seed)
+    q, k = rnd(g, T, heads, 64, std=0.5, dtype=BF16), rnd(g, T, heads, 64, std=0.5, dtype=BF16)
+    q[:, :, 0] = 8.0
+    # scale log2(e) q.k = 0.125 x 1.4427 x 8 k_0
+    k[:, :, 0] = ((torch.arange(T) // 64).float() * (step / (0.125 * 1.4427 * 8.0)))[:, None].to(BF16)
+    return q, k, rnd(g, T, heads, 64, dtype=BF16)
+
+
+@pytest.mark.parametrize("lengths", [(64 * 9 + 5,), (577, 130, 300)])
+def test_a_maximum_that_moves_in_every_tile(ctx, lengths):      # noqa: F811
+    """The tile's P with the old maximum, 2^14 and more too large, may not stay where the new one belongs.  Every one of
+    40 launches is the formula's, and has the first one's bits."""
+    offsets = [0]
+    for n in lengths:
+        offsets.append(offsets[-1] + n)
+    q, k, v = growing(offsets[-1], 3, 21)
+    want, want_lse = ref.packed(d64(q), d64(k), d64(v), offsets)
+    bound = ref.packed_bounds(d64(q), d64(k), d64(v), torch.zeros_like(want), offsets)["o"]
+    at = torch.tensor(offsets, dtype=torch.int32, device="cuda")
+    dev = [t.cuda() for t in (q, k, v)]
+    outs = [ctx.lasad_packed_attention(*dev, at, want_lse=True) for _ in range(40)]
+    assert ctx.device_status() == 0
+    inside("o", outs[0][0], want, bound)
+    near(outs[0][1], want_lse, F32, "lse", extra=2.0 ** -18)
+    for o, lse in outs[1:]:
+        assert torch.equal(o, outs[0][0]) and torch.equal(lse, outs[0][1])
+
+
+def test_every_launch_of_many_has_the_same_bits(ctx):      # noqa: F811
+    """Forward and gradient back to back, ordinary scores and growing ones: each launch against the first."""
+    g = gen(22)
+    T = 1300
+    at = torch.tensor([0, 700, 701, T], dtype=torch.int32, device="cuda")
+    for q, k, v in ((rnd(g, T, 4, 64, std=1.5, dtype=BF16), rnd(g, T, 4, 64, dtype=BF16), rnd(g, T, 4, 64, dtype=BF16)), growing(T, 4, 23)):
+        q, k, v, do = (t.cuda() for t in (q, k, v, rnd(g, T, 4, 64, dtype=BF16)))
+        first, same = None, torch.ones((), dtype=torch.bool, device="cuda")
+        for _ in range(30):
+            o, lse = ctx.lasad_packed_attention(q, k, v, at, want_lse=True)
+            got = (o, lse) + ctx.lasad_packed_attention_backward(q, k, v, o, lse, do, at)
+            first = first or got
+            for a, b in zip(first, got):
+                same &= (a == b).all()
+        assert bool(same) and ctx.device_status() == 0

@@ -397,7 +397,8 @@ __device__ __forceinline__ void softmax_rows(const Params& p, Smem& sm, int g, i
                         for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
                         tmem_st16(at_o + 16 * c, o);
                     }
-                    exponentials(sv, p.scale2, -m, at_p, l);
+                    // (a row of the warp may still have seen nothing but -infinity)
+                    exponentials(sv, p.scale2, m == -INFINITY ? 0.0f : -m, at_p, l);
                 }
             }
             // values past the sequence's end do not count, whatever they are

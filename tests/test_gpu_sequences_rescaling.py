@@ -5,10 +5,9 @@ import math
 import pytest
 import torch
 
-from paper_2507_01652_b200 import binding  # noqa: F401
 from tests import _sequences_ref as ref
 from tests.test_gpu_mixers import BF16, F32, ctx, d64, gen, near, rnd  # noqa: F401
-from tests.test_gpu_sequences import inside
+from tests.test_gpu_sequences import both_ways, inside
 
 pytestmark = pytest.mark.gpu
 
@@ -58,3 +57,44 @@ def test_every_launch_of_many_has_the_same_bits(ctx):      # noqa: F811
             for a, b in zip(first, got):
                 same &= (a == b).all()
         assert bool(same) and ctx.device_status() == 0
+
+
+def unseen(seed, first):
+    """Two sequences of keys and queries: row 200 of the first (with 31 others in its warp) has scores of -infinity, by
+    overflow, with the keys before ``first``; the other rows do not see that channel of the keys.  Row 203's scores grow
+    by about 40 (in log2) with key 70, of the second tile."""
+    g = gen(seed)
+    n, T = 320, 420
+    q, k, v = (rnd(g, T, h, 64, std=0.5, dtype=BF16) for h in (2, 1, 1))
+    q[:, :, :2] = 0.0
+    k[:, :, :2] = 0.0
+    k[:first, :, 0] = -1e30
+    q[200, :, 0] = 1e30
+    k[70, :, 1], q[203, :, 1] = 16.0, 14.0
+    do = rnd(g, T, 2, 64, dtype=BF16)
+    return [q, k, v, do], [0, n, T]
+
+
+@pytest.mark.parametrize("first", [128, 201])
+def test_a_row_that_has_seen_nothing_beside_one_that_grows(ctx, first):      # noqa: F811
+    """Scores that overflow are -infinity, and weigh nothing: row 200's output is that of the keys it does see, and 0 with
+    lse -infinity where there are none, whatever its neighbours do and on both implementations."""
+    (q, k, v, do), offsets = unseen(31, first)
+    at = torch.tensor(offsets, dtype=torch.int32, device="cuda")
+    seen = k.clone()
+    seen[:, :, 0] = 0.0
+    other = q.clone()
+    other[200, :, 0] = 0.0
+    want, want_lse = ref.packed(d64(other), d64(seen), d64(v), offsets)
+    bounds = ref.packed_bounds(d64(other), d64(seen), d64(v), d64(do), offsets)
+    n = 201 - first
+    if n:                                         # row 200 as the last row of a sequence of the keys that it sees
+        part = [d64(t)[first:201] for t in (other, seen, v, do)]
+        o, lse = ref.packed(*part[:3], [0, n])
+        want[200], want_lse[:, 200] = o[-1], lse[:, -1]
+        bounds["o"][200] = ref.packed_bounds(*part, [0, n])["o"][-1]
+    else:
+        want[200], want_lse[:, 200], bounds["o"][200] = 0.0, -math.inf, 0.0
+    for way in both_ways(ctx, [t.cuda() for t in (q, k, v, do)], at):
+        inside("o", way[0], want, bounds["o"])
+        near(way[1], want_lse, F32, "lse", extra=2.0 ** -18)

@@ -98,3 +98,19 @@ def test_a_row_that_has_seen_nothing_beside_one_that_grows(ctx, first):      # n
     for way in both_ways(ctx, [t.cuda() for t in (q, k, v, do)], at):
         inside("o", way[0], want, bounds["o"])
         near(way[1], want_lse, F32, "lse", extra=2.0 ** -18)
+
+
+@pytest.mark.parametrize("n", [513, 577, 70])
+def test_rows_behind_a_sequence_do_not_move_its_maximum(ctx, n):      # noqa: F811
+    """A warp's last rows may belong to another sequence or to none.  Theirs have scores of hundreds here, so their
+    maxima move in tile after tile; the sequence's own rows get the bits that they get alone."""
+    g = gen(41)
+    T = 800
+    q, k, v = (rnd(g, T, h, 64, std=s, dtype=BF16) for h, s in ((4, 1.5), (2, 1.0), (2, 1.0)))
+    q[n:] *= 60.0
+    dev = [t.cuda() for t in (q, k, v)]
+    alone = ctx.lasad_packed_attention(*[t[:n].contiguous() for t in dev], torch.tensor([0, n], dtype=torch.int32, device="cuda"), want_lse=True)
+    for offsets in ([0, n, T], [0, n]):
+        o, lse = ctx.lasad_packed_attention(*dev, torch.tensor(offsets, dtype=torch.int32, device="cuda"), want_lse=True)
+        assert torch.equal(o[:n], alone[0]) and torch.equal(lse[:, :n], alone[1])
+    assert ctx.device_status() == 0

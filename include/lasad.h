@@ -447,8 +447,9 @@ int lasad_window_cache_store(lasad_ctx* ctx, const lasad_window_params* p, const
  *   has rows offsets[i] .. offsets[i + 1] - 1 (none where they are equal).  A row that no sequence has (behind the
  *   last one) is empty: its o and gradients are 0 and its lse is -infinity, and nothing that stands in q, k,
  *   v, o, do there counts, not even a NaN.  Nor does a row of one sequence count in another's.  (Inside a sequence a
- *   NaN or an infinity may reach rows ahead of it: a weight of 0 times an infinity is not 0.)  Offsets that do not
- *   ascend give undefined results, but no access outside the N rows.
+ *   NaN or an infinity may reach rows ahead of it: a weight of 0 times an infinity is not 0.)  A row whose scores are
+ *   all -infinity, by overflow of fp32 too, is empty as well.  Offsets that do not ascend give undefined results, but no
+ *   access outside the N rows.
  *   lse [Hq,N] fp32: log of the row's sum of e^(scale q.k); may be NULL in the forward.
  * Arithmetic and rounding are those of lasad_window_attention (bf16: tensor cores, weights and the gradients of the
  * scores in bf16 where they enter a product; f32 and LASAD_OPT_WINDOW_IMPL = 1: fp32).

@@ -63,6 +63,9 @@ __device__ __forceinline__ Region region_of(const int* offsets, int S, int N, in
     r.owned = lo > 0 && lo <= S;
     return r;
 }
+// What a row's scores are moved by in the gradient, -lse log2(e).  A row that has seen nothing but scores of -infinity is empty,
+// and so are its weights: no -infinity + infinity.
+__device__ __forceinline__ float minus_lse(float lse) { return lse == -INFINITY ? lse : lse * -1.4426950408889634f; }
 #endif
 
 // The gradient's workspace: of each row -lse log2(e) and -Delta, Delta_t = do_t.o_t, in blocks of 64 rows of a

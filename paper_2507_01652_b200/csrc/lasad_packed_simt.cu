@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(kThreads) packed_dq_simt_kernel(const PackedAr
         sum += __shfl_xor_sync(0xffffffffu, sum, 1);
         sum += __shfl_xor_sync(0xffffffffu, sum, 2);
         if (part == 0) {
-            const float lse = q0 + row < len ? -a.lse[(long long)h * a.N + r.start + q0 + row] * kLog2e : 0.0f;
+            const float lse = q0 + row < len ? minus_lse(a.lse[(long long)h * a.N + r.start + q0 + row]) : 0.0f;
             sm.lse[row] = lse;
             sm.delta[row] = -sum;
             float* stat = a.ws + packed_stat_at(a, h, number);

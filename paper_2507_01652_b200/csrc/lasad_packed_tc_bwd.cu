@@ -256,7 +256,7 @@ packed_backward_tc_kernel(const __grid_constant__ CUtensorMap tm_y1, const __gri
         float row_lse = 0.0f, row_delta = 0.0f, rest[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         if (!KEYS) {
             if (group == 1) half_row(p.o + at_row * p.os[0] + h * p.os[1] + 32 * c, mine, ov);
-            if (r < len) row_lse = -p.lse[(long long)h * p.N + at_row] * kLog2e;
+            if (r < len) row_lse = minus_lse(p.lse[(long long)h * p.N + at_row]);
         }
         tmem_st16(lanes + (group == 0 ? kColX1 : kColX2) + 16 * c, xv);
         tmem_wait_st();

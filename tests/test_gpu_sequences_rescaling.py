@@ -114,3 +114,24 @@ def test_rows_behind_a_sequence_do_not_move_its_maximum(ctx, n):      # noqa: F8
         o, lse = ctx.lasad_packed_attention(*dev, torch.tensor(offsets, dtype=torch.int32, device="cuda"), want_lse=True)
         assert torch.equal(o[:n], alone[0]) and torch.equal(lse[:, :n], alone[1])
     assert ctx.device_status() == 0
+
+
+def test_the_gradient_of_a_row_that_has_seen_nothing(ctx):      # noqa: F811
+    """Such a row is empty (o 0, lse -infinity): its gradient is 0, and nothing of it comes to its keys and values."""
+    (q, k, v, do), offsets = unseen(32, 201)
+    at = torch.tensor(offsets, dtype=torch.int32, device="cuda")
+    leaves = [d64(t) for t in (q, k, v)]
+    leaves[0][200, :, 0] = 0.0
+    leaves[1][:, :, 0] = 0.0
+    leaves = [t.requires_grad_() for t in leaves]
+    without = do.clone()
+    without[200] = 0.0                            # (then nothing comes from the row)
+    want = torch.autograd.grad(ref.packed(*leaves, offsets)[0], leaves, d64(without))
+    bounds = ref.packed_bounds(*[t.detach() for t in leaves], d64(without), offsets)
+    for way in both_ways(ctx, [t.cuda() for t in (q, k, v, do)], at):
+        assert bool((way[2][200] == 0).all())
+        for name, got, w in zip(("dq", "dk", "dv"), way[2:], want):
+            got, w, b = got.clone(), w.clone(), bounds[name]
+            if name == "dq":
+                got[:, :, 0], w[:, :, 0] = 0.0, 0.0      # (dq_0 is ds k_0, ...)
+            inside(name, got, w, b)

@@ -435,7 +435,8 @@ int lasad_window_cache_store(lasad_ctx* ctx, const lasad_window_params* p, const
  * A layer that attends to whole sequences: prompts and training on packed sequences, a paged cache in 8 bits,
  * and one token per sequence against it.  The rules are those of the calls above (alignment, strides, dtypes,
  * workspaces, graphs, the same bits on every run); d in {32, 64}, Hk divides Hq, query head h reads key head
- * h / (Hq / Hk).
+ * h / (Hq / Hk).  An output, a pool that is appended to among them, has no element in two places: in order of
+ * size, each stride (of a dimension longer than 1) is at least what the smaller ones span.
  * ---------------------------------------------------------------------------------------------- */
 
 /*

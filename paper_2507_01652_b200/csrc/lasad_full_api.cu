@@ -28,13 +28,32 @@ bool on_device(const lasad_ctx* ctx)
     int current = -1;
     return cudaGetDevice(&current) == cudaSuccess && current == ctx->device;
 }
-// Strides of (row, head): whole 16 bytes, none that lets two elements share memory.
-bool rows_ok(const int64_t* s, int64_t esz, int N, int H, int d, long long (&to)[2])
+// Whether runs of `size` elements at these strides share no memory, one dimension inside another: sorted by stride, each steps
+// over all that the ones before it span.  (Layouts that interleave in another way are refused with those that overlap.)
+template <int NDIM> bool apart(const int64_t* stride, const int (&extent)[NDIM], int size)
+{
+    int order[NDIM], n = 0;
+    for (int i = 0; i < NDIM; ++i) {
+        if (extent[i] < 2) continue;
+        int at = n++;
+        for (; at > 0 && stride[order[at - 1]] > stride[i]; --at) order[at] = order[at - 1];
+        order[at] = i;
+    }
+    __int128 span = size;
+    for (int i = 0; i < n; ++i) {
+        if (stride[order[i]] < span) return false;
+        span += (__int128)stride[order[i]] * (extent[order[i]] - 1);
+    }
+    return true;
+}
+// Strides of (row, head): whole 16 bytes, none that repeats a row; those of an output lead to no element twice.
+bool rows_ok(const int64_t* s, int64_t esz, int N, int H, int d, bool output, long long (&to)[2])
 {
     for (int i = 0; i < 2; ++i) {
-        if (s[i] < 0 || (s[i] * esz) % 16 != 0) return false;
+        if (s[i] < 0 || s[i] % (16 / esz) != 0) return false;
         to[i] = s[i];
     }
+    if (output) return apart(s, {N, H}, d);
     return (s[0] > 0 || N == 1) && (s[1] >= d || H == 1);
 }
 bool heads_ok(int Hq, int Hk, int d) { return Hq > 0 && Hk > 0 && d > 0 && Hq % Hk == 0; }
@@ -49,7 +68,8 @@ int packed_args(lasad_ctx* ctx, const lasad_packed_params* p, bool backward, las
         {p->q_stride, a.qs, p->Hq}, {p->k_stride, a.ks, p->Hk}, {p->v_stride, a.vs, p->Hk}, {p->o_stride, a.os, p->Hq},
         {p->do_stride, a.dos, p->Hq}, {p->dq_stride, a.dqs, p->Hq}, {p->dk_stride, a.dks, p->Hk}, {p->dv_stride, a.dvs, p->Hk}};
     for (int i = 0; i < (backward ? 8 : 4); ++i)
-        if (!rows_ok(tensors[i].s, p->dtype == LASAD_F32 ? 4 : 2, p->N, tensors[i].H, p->d, tensors[i].to)) return LASAD_ERR_INVALID_ARG;
+        if (!rows_ok(tensors[i].s, p->dtype == LASAD_F32 ? 4 : 2, p->N, tensors[i].H, p->d, i == (backward ? 5 : 3) || i > 5, tensors[i].to))
+            return LASAD_ERR_INVALID_ARG;
     if ((p->d != 32 && p->d != 64) || p->N > (1 << 30) || p->S > 65535) return LASAD_ERR_UNSUPPORTED;
     // (the tiles of all heads are counted in 32 bits)
     if (lasad::region_tiles(p->N, p->S, lasad::kStatRows) * p->Hq > 0x7fffffffLL) return LASAD_ERR_UNSUPPORTED;
@@ -70,13 +90,14 @@ int packed_impl(const lasad_ctx* ctx, const lasad::PackedArgs& a)
     return ctx->opt_window_impl == 2 && !a.bf16 ? LASAD_ERR_UNSUPPORTED : ctx->opt_window_impl;
 }
 
-// Strides in bytes of (page, head, slot).
-bool pages_ok(const int64_t* s, const lasad_paged_params* p, long long (&to)[3])
+// Strides in bytes of (page, head, slot), with the rules of rows_ok.
+bool pages_ok(const int64_t* s, const lasad_paged_params* p, bool output, long long (&to)[3])
 {
     for (int i = 0; i < 3; ++i) {
         if (s[i] < 0 || s[i] % 16 != 0) return false;
         to[i] = s[i];
     }
+    if (output) return apart(s, {p->pages, p->Hk, p->page}, p->d);
     return (s[0] > 0 || p->pages == 1) && (s[1] >= p->d || p->Hk == 1) && s[2] >= p->d;
 }
 // Whether a head's last slot of the last page begins less than 2^32 - 1 times 16 bytes behind its first of the first.
@@ -96,10 +117,11 @@ int paged_args(lasad_ctx* ctx, const lasad_paged_params* p, bool append, bool qu
     if (!append && !std::isfinite(p->scale)) return LASAD_ERR_INVALID_ARG;
     const int64_t esz = p->dtype == LASAD_F32 ? 4 : 2;
     const int rows = append ? p->N : p->B;
-    if (!pages_ok(p->k_pages_stride, p, a.kps) || !pages_ok(p->v_pages_stride, p, a.vps)) return LASAD_ERR_INVALID_ARG;
-    if (append && (!rows_ok(p->k_stride, esz, rows, p->Hk, p->d, a.ks) || !rows_ok(p->v_stride, esz, rows, p->Hk, p->d, a.vs)))
+    if (!pages_ok(p->k_pages_stride, p, append, a.kps) || !pages_ok(p->v_pages_stride, p, append, a.vps)) return LASAD_ERR_INVALID_ARG;
+    if (append && (!rows_ok(p->k_stride, esz, rows, p->Hk, p->d, false, a.ks) || !rows_ok(p->v_stride, esz, rows, p->Hk, p->d, false, a.vs)))
         return LASAD_ERR_INVALID_ARG;
-    if (queries && (!rows_ok(p->q_stride, esz, rows, p->Hq, p->d, a.qs) || !rows_ok(p->o_stride, esz, rows, p->Hq, p->d, append ? a.qos : a.os)))
+    if (queries && (!rows_ok(p->q_stride, esz, rows, p->Hq, p->d, false, a.qs) ||
+                    !rows_ok(p->o_stride, esz, rows, p->Hq, p->d, true, append ? a.qos : a.os)))
         return LASAD_ERR_INVALID_ARG;
     if ((p->d != 32 && p->d != 64) || (p->page != 16 && p->page != 32 && p->page != 64 && p->page != 128) || p->B > 65535 ||
         (int64_t)p->table_pages * p->page > (1 << 30))

@@ -343,7 +343,9 @@ window_forward_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
                 tc_fence_after();
                 const bool grow = top > m + 8.0f || (m == -INFINITY && top > m);
                 if (i == 0) {
-                    m = top;
+                    // (rows behind the sequence's end may hold anything and must not decide when these move: nothing grows
+                    // over theirs)
+                    m = t < u.len ? top : INFINITY;
                 } else if (__any_sync(0xffffffffu, grow)) {
                     // (every row of the warp moves to its maximum now, or its turn would come one by one: 25 % of
                     // the steps scaled where only rows that had grown moved)

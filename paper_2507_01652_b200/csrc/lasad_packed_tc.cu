@@ -16,13 +16,14 @@
 // takes the same places' turn, so S being there says that P's place is free.  And the maximum is not waited for:
 // P is formed with the m that the row has, its maximum beside it; only where that has grown by more than 8 (a factor
 // 2^8, far inside the range of fp32 and bf16; after the first tiles rare) m moves, O and l are scaled and P is formed
-// again.
+// again, behind a wait for the first one's stores.
 //
-// Measured: 1 x 9217 tokens, 24 query and 8 key heads: 418 us, 624 TFLOP/s of the pairs that count, the pipe of the
-// exponentials issuing on 56 % of the clocks; 64 sequences of 1 to 577 tokens, 16 and 4 heads: 61 us.  With clocks read
-// in the loop (which slows it a little) a group alone takes 1290 clocks for a tile, 740 of them from the scores to P, the two
-// groups together 1775 to 1800 for two tiles: they meet in the exponentials, also when one is made to start late (424 to
-// 450 us).  Tried on that case: 128-key tiles 421, with a quarter of the exponentials as polynomials 412 (tiles of 64 with an
+// Measured: 1 x 9217 tokens, 24 query and 8 key heads: 421 to 424 us, 617 TFLOP/s of the pairs that count, the pipe of the
+// exponentials issuing on 56 % of the clocks; 64 sequences of 1 to 577 tokens, 16 and 4 heads: 61.5 us (d = 32, at d = 64's
+// width: 421 and 60).  With clocks read in the loop (which slows it a little) a group alone takes 1290 clocks for a tile,
+// 740 of them from the scores to P, the two groups together 1775 to 1800 for two tiles: they meet in the exponentials, also
+// when one is made to start late (424 to 450 us).  Tried on that case, where a form without the care for empty rows and
+// for rows behind the sequence's end took 418: 128-key tiles 421, with a quarter of the exponentials as polynomials 412 (tiles of 64 with an
 // eighth, a quarter, three eighths: 429, 419, 444); sixteen warps on even and odd tiles 417; three groups 450 (and 83
 // instead of 61 us on the short sequences); S issued right behind the product 429; masked and other tiles as two
 // bodies 443; a short rolled body 462.

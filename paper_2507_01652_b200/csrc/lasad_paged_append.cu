@@ -16,11 +16,12 @@
 // that would be a step of 1/16.  (fp64 multiply-adds run at half of the fp32 rate here.)  Queries turn in 32
 // bits and go back to their own type.
 //
-// Bound by memory: k, v and q in, a byte a value and q out.  Prompts: a page's keys, or values, of some heads for a team of
+// Bound by memory where prompts are long: k, v and q in, a byte a value and q out.  Prompts: a page's keys, or values, of some heads for a team of
 // page / 16 warps, so that its maximum needs no second reading, the next head's rows on their way meanwhile; queries by CTAs of
 // their own, eight heads at a time (8 x 9217 tokens, 24 query and 8 key heads, 680 MB: 139 us, 4.9 TB/s; four heads at a time 154;
-// keys, then values, by the same warps and one query head at a time 326).  One token per sequence: 3.8 us for 256 x 20 heads (by the prompts'
-// kernel 11.6).
+// keys, then values, by the same warps and one query head at a time 326; fp32, 1284 MB: 236).  64 prompts of 1 to 577 tokens, 16 and 4
+// heads, 104 MB: 31.5 us, 3.3 TB/s; the search for a row's sequence is little of that, as the same tokens of 8 sequences
+// take 29.3 and of one 28.6.  One token per sequence: 3.9 us for 256 x 20 heads (by the prompts' kernel 11.6).
 #include "lasad_full.cuh"
 #include "lasad_tc_ptx.cuh"
 
